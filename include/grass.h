@@ -453,6 +453,117 @@ grass_status grass_adam_scatter_replayable(const float* GC, int64_t ldgc, void* 
                                            void* stream);
 
 /* ---------------------------------------------------------------------------
+ * The norms in front of the linear layers (what produces X, and what dX of the linear layers
+ * goes through next).  For every token t, with h the row that is normed:
+ *   h = X[t, :]                    or, with a residual branch R, X[t, :] + R[t, :] rounded to `dt`
+ *   LAYER: mu = mean(h), s = 1 / sqrt(mean((h - mu)^2) + eps)
+ *   RMS:   mu = 0,       s = 1 / sqrt(mean(h^2) + eps)
+ *   Y[t, :] = (h - mu) * s * gain + bias, rounded once to `dt`.
+ * X, R, H, Y: T x n of dtype `dt` with leading dimensions of their own; gain, bias: n values of
+ * dtype `gdt` (NULL: ones, zeros).  R NULL: no residual branch, H is not written; else H receives
+ * h.  mean, rstd: NULL, or T floats that receive mu and s for the backward pass (mean is not
+ * written by RMS).  Sums are fp32 (sums of squares therefore below 2^128); a NaN or an infinity
+ * spoils its own row and no other.  H may be X or R, and Y may be X or R (the same address
+ * and leading dimension; not H); other overlaps are not allowed.  T = 0 is a no-op; n >= 1.
+ * Errors: NULL, SHAPE (also eps negative or NaN), DTYPE. */
+typedef enum { GRASS_NORM_LAYER = 0, GRASS_NORM_RMS = 1 } grass_norm;
+grass_status grass_norm_forward(grass_norm kind, const void* X, int64_t ldx, const void* R,
+                                int64_t ldr, grass_dtype dt, int64_t T, int64_t n, const void* gain,
+                                const void* bias, grass_dtype gdt, float eps, void* H, int64_t ldh,
+                                void* Y, int64_t ldy, float* mean, float* rstd, void* stream);
+
+/* Backward pass of grass_norm_forward, from what it read as h (H; X where there was no residual
+ * branch) and the mean and rstd that it kept:
+ *   xh = (h - mean) * rstd, z = dY * gain          (mean is not read by RMS and taken as 0)
+ *   dX = rstd * (z - mean_n(z) - xh * mean_n(z * xh)) [+ dR]       (RMS: without mean_n(z))
+ *   dgain = sum_t dY * xh,   dbias = sum_t dY                      (n floats each)
+ * dR: NULL, or the gradient that reaches h by its other way (the residual stream), added in fp32
+ * before dX is rounded once; dX is the gradient of X and of R alike.  dgain, dbias: NULL where not
+ * wanted.  dX may be dY, H or dR (the same address and leading dimension).  The sums over t are
+ * fp32, in an order that depends on the sizes alone, so that equal calls give equal bits.  `ws` must
+ * hold grass_norm_backward_workspace(...) bytes (NULL where neither dgain nor dbias is wanted).
+ * T = 0 writes zeros to dgain and dbias; n >= 1.
+ * Errors: NULL, SHAPE, DTYPE, WORKSPACE. */
+size_t grass_norm_backward_workspace(int64_t T, int64_t n, grass_dtype dt);
+grass_status grass_norm_backward(grass_norm kind, const void* dY, int64_t lddy, const void* H,
+                                 int64_t ldh, const void* dR, int64_t lddr, grass_dtype dt, int64_t T,
+                                 int64_t n, const void* gain, grass_dtype gdt, const float* mean,
+                                 const float* rstd, void* dX, int64_t lddx, float* dgain,
+                                 float* dbias, void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * AdamW over many tensors at once: the parameters that no projection covers (embeddings, output
+ * head, gains and biases of the norms).  For every element, in fp32, each product and sum of the
+ * moments rounded by itself:
+ *   g = G * grad_scale     m = b1*m + (1-b1)*g     v = b2*v + ((1-b2)*g)*g
+ *   W = W * (1 - lr*weight_decay) - lr * (m / (1-b1^t)) / (sqrt(v / (1-b2^t)) + eps)
+ * W is rounded once to its dtype.  The moments are fp32, or 8 bits each (GRASS_MOMENTS_Q8): M holds
+ * e4m3 and V e5m2 values (OCP forms), and each block of 128 elements, counted from the tensor's
+ * start, has a scale in mscale / vscale ((elems + 127) / 128 floats each): 2^(e-7) and 2^(e-14), e the
+ * exponent of the block's largest finite magnitude, at least -103.  The new moments, in fp32, give
+ * the update and are then stored: x / scale becomes the multiple floor(x / step + u) of the type's
+ * step at x, where u, from [0, 1), is the top 20 (M) or 21 (V) bits of the 32-bit word
+ * j * 0x9E3779B1 + t * c, j the element's place in its block and c = 0x6A09E667 (M) or
+ * 0xBB67AE85 (V).  Over the steps u takes every part of [0, 1) alike, so what one step's rounding
+ * takes another gives back: rounded to the nearest value, V would stop following a gradient that
+ * changes it by less than an eighth a step, which is every gradient at b2 = 0.999.  A moment that is not finite is
+ * stored as NaN; the other elements of its block are not affected.  A block of zeros (state at the
+ * start: all codes zero, scales of any finite value) is exact.
+ *
+ * The tensors are laid out once into a plan, which the caller copies to device memory and passes to
+ * every step: grass_adamw_plan_bytes says how large it is, grass_adamw_plan writes it into `plan`
+ * (HOST memory) and fills `layout` (kept on the host; every later call needs both).  A plan holds the tensors' addresses: lay
+ * it out anew where they change.  A tensor is rows x cols with leading dimensions ldw and ldg of W and
+ * G; M and V are dense.  With 8-bit moments and a leading dimension that is not cols, cols must be a
+ * multiple of 128 (unless rows is 1).  A plan whose tensors name only G (W, M and V NULL) serves grass_grad_norm
+ * alone.  Tensors must not overlap.  count = 0 and tensors without elements are legal.
+ * Errors: NULL, SHAPE (also an address that is not a multiple of its type's size), DTYPE,
+ * WORKSPACE (plan_bytes too small). */
+typedef enum { GRASS_MOMENTS_F32 = 0, GRASS_MOMENTS_Q8 = 1 } grass_moments;
+typedef struct {
+    void* W;             /* rows x cols weights of dtype wdt, updated in place           */
+    const void* G;       /* their gradients, dtype gdt                                   */
+    void* M;             /* rows * cols moments, updated in place                        */
+    void* V;
+    float* mscale;       /* scales of 8-bit moments (ignored for fp32 moments)           */
+    float* vscale;
+    int64_t rows, cols;
+    int64_t ldw, ldg;
+    grass_dtype wdt, gdt;
+    grass_moments moments;
+    float weight_decay;
+} grass_adamw_tensor;
+#define GRASS_ADAMW_GROUPS 10
+typedef struct {
+    int64_t chunks[GRASS_ADAMW_GROUPS]; /* pieces of work for each combination of types, in the plan's order */
+} grass_adamw_layout;
+size_t grass_adamw_plan_bytes(int count, const grass_adamw_tensor* tensors);
+grass_status grass_adamw_plan(int count, const grass_adamw_tensor* tensors, void* plan,
+                              size_t plan_bytes, grass_adamw_layout* layout);
+
+/* One step over a plan (device memory, 16-byte aligned).  t >= 1 is the 1-based count of steps.
+ * step_scalars: NULL, or a device array of the 4 floats of grass_adamw_step_scalars, which replace lr and
+ * t (for captured steps; the fourth is t modulo 2^24, which the thresholds are formed from in either
+ * case).  grad_scale: NULL (1), or a device float that every gradient is multiplied by, such as
+ * the factor of grass_grad_norm; where it is NaN the step changes nothing.
+ * Errors: NULL, SHAPE (also t < 1, a beta outside [0,1), a plan of gradients alone), DEVICE. */
+grass_status grass_adamw_step(const void* plan, const grass_adamw_layout* layout, float lr,
+                              float beta1, float beta2, float eps, int64_t t,
+                              const float* step_scalars, const float* grad_scale, void* stream);
+grass_status grass_adamw_step_scalars(float lr, float beta1, float beta2, int64_t t,
+                                      float* scalars);
+
+/* Global norm of the gradients of a plan, and the factor that clips it:
+ *   out[0] = sqrt(sum of G^2 over all tensors),   out[1] = min(1, max_norm / out[0])
+ * (out: 2 device floats; sums in fp64, in a fixed order).  Where the sum is not finite out[1] is NaN,
+ * which makes grass_adamw_step skip the step.  No gradients: 0 and 1.  `ws` must hold
+ * grass_grad_norm_workspace(layout) bytes, 8-byte aligned.
+ * Errors: NULL, SHAPE (also max_norm negative or NaN), WORKSPACE. */
+size_t grass_grad_norm_workspace(const grass_adamw_layout* layout);
+grass_status grass_grad_norm(const void* plan, const grass_adamw_layout* layout, float max_norm,
+                             float* out, void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
  * Test hooks.  The launchers choose their kernels from the shapes and alignments of a call;
  * tests need to reach every kernel with small inputs, so a process-wide override exists for
  * each such choice.  value 0 (the initial state) leaves the choice to the library.  The

@@ -1,0 +1,387 @@
+// grass_adamw_plan, grass_adamw_step, grass_grad_norm: AdamW and the gradients' norm over many tensors.
+//
+// All of it is bound by memory: every array is read once and written once.  The plan cuts the
+// tensors into chunks of 2048 elements and holds for each the addresses where it starts, so that a
+// workgroup finds its work with one 64-byte load whatever the number and sizes of the tensors;
+// chunks of one combination of types lie together and take one launch.  A thread handles eight
+// consecutive elements.  The 16 lanes that hold a block of 128 lie in one row of a wavefront, whose
+// lanes exchange values without LDS.
+#include "adam.hpp"
+#include "elem8.hpp"
+
+namespace grass {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kChunk = kThreads * 8;
+constexpr int kQBlock = 128;  // elements that share a scale
+
+struct alignas(16) Chunk {
+    void* W;
+    const void* G;
+    void* M;
+    void* V;
+    float* mscale;
+    float* vscale;
+    int32_t elems;
+    int32_t gdt;
+    float weight_decay;
+    int32_t unused;
+};
+static_assert(sizeof(Chunk) == 64, "one load of sixteen dwords");
+
+constexpr int kStepGroups = 8;  // by W's, G's and the moments' type; two more for gradients alone
+
+int group_of(const grass_adamw_tensor& a) {
+    if (!a.W) return kStepGroups + (a.gdt == GRASS_F32 ? 0 : 1);
+    return (a.wdt == GRASS_F32 ? 0 : 4) + (a.gdt == GRASS_F32 ? 0 : 2) + (a.moments == GRASS_MOMENTS_F32 ? 0 : 1);
+}
+
+// The pieces a tensor is cut into: itself where its rows follow one another, else its rows.
+struct Pieces {
+    int64_t count, elems;
+};
+Pieces pieces_of(const grass_adamw_tensor& a) {
+    const bool dense = a.rows <= 1 || (a.ldg == a.cols && (!a.W || a.ldw == a.cols));
+    if (a.rows == 0 || a.cols == 0) return {0, 0};
+    return dense ? Pieces{1, a.rows * a.cols} : Pieces{a.rows, a.cols};
+}
+
+struct StepArgs {
+    const Chunk* chunks;
+    AdamParams adam;
+    uint32_t t;
+    const float* grad_scale;
+};
+
+// Moments of eight elements: fp32 ...
+struct MomentsF32 {
+    float m[8], v[8];
+    __device__ __forceinline__ void load(const Chunk& c, int at, int left) {
+        Raw8<float> a, b;
+        const float *pm = static_cast<const float*>(c.M) + at, *pv = static_cast<const float*>(c.V) + at;
+        if (left >= 8) {
+            a.load_once(pm);
+            b.load_once(pv);
+        } else {
+            a.load_some(pm, left);
+            b.load_some(pv, left);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            m[i] = a.get(i);
+            v[i] = b.get(i);
+        }
+    }
+    __device__ __forceinline__ void store(const Chunk& c, int at, int left, uint32_t) const {
+        Raw8<float> a, b;
+        a.set(m);
+        b.set(v);
+        float *pm = static_cast<float*>(c.M) + at, *pv = static_cast<float*>(c.V) + at;
+        if (left >= 8) {
+            a.store_once(pm);
+            b.store_once(pv);
+        } else {
+            a.store_some(pm, left);
+            b.store_some(pv, left);
+        }
+    }
+};
+
+typedef uint32_t raw2_t __attribute__((ext_vector_type(2)));
+typedef raw2_t raw2_on1_t __attribute__((aligned(1)));
+
+// The largest of the 16 lanes of a row, in every one of them.
+template <int kRotate>
+__device__ __forceinline__ uint32_t row_rotate(uint32_t x) {
+    return static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(x), 0x120 + kRotate, 0xF, 0xF, true));
+}
+__device__ __forceinline__ uint32_t row_max(uint32_t x) {
+    x = max(x, row_rotate<8>(x));
+    x = max(x, row_rotate<4>(x));
+    x = max(x, row_rotate<2>(x));
+    return max(x, row_rotate<1>(x));
+}
+
+constexpr uint32_t kInf = 0x7F800000u;
+
+// One kind of 8-bit moment: kMan bits of mantissa, scale 2^(e - kTop).  Scaled by a further
+// 2^(bias - 127) the type's numbers, subnormal ones too, are the fp32 numbers whose bits are the code
+// followed by zeros; so a value becomes a code by cutting its bits after adding u's bits to them.
+template <int kMan, int kTop, int kBias>
+struct Code8 {
+    static constexpr int kCut = 23 - kMan;
+    // what the eight lanes' values allow as a scale (all 16 lanes of the block get the same)
+    __device__ static __forceinline__ uint32_t exponent(const float (&x)[8]) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t b = __float_as_uint(x[i]) & 0x7FFFFFFFu;
+            top = max(top, b < kInf ? b : 0u);
+        }
+        return max(row_max(top) >> 23, 24u);
+    }
+    __device__ static __forceinline__ float scale(uint32_t e) { return __uint_as_float((e - kTop) << 23); }
+    __device__ static __forceinline__ uint32_t code(float x, float inv_scale, uint32_t word) {
+        const float y = (x * inv_scale) * __uint_as_float(kBias << 23);
+        const uint32_t b = __float_as_uint(x);
+        const uint32_t c = ((__float_as_uint(y) & 0x7FFFFFFFu) + (word >> (32 - kCut))) >> kCut;
+        return ((b & 0x7FFFFFFFu) < kInf ? c : 0x7Fu) | (b >> 31 << 7);
+    }
+    // the eight lanes' codes; word: u's bits at the first of them
+    __device__ static __forceinline__ raw2_t codes(const float (&x)[8], uint32_t e, uint32_t word) {
+        const float inv = __uint_as_float((254u + kTop - e) << 23);
+        raw2_t r = {0, 0};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r[i / 4] |= code(x[i], inv, word + i * 0x9E3779B1u) << (8 * (i & 3));
+        return r;
+    }
+};
+typedef Code8<3, 7, 7> CodeM;     // e4m3
+typedef Code8<2, 14, 15> CodeV;   // e5m2
+
+__device__ __forceinline__ raw2_t load_codes(const void* p, int at, int left) {
+    const uint8_t* q = static_cast<const uint8_t*>(p) + at;
+    if (left >= 8) return __builtin_nontemporal_load(reinterpret_cast<const raw2_on1_t*>(q));
+    raw2_t r = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < left) r[i / 4] |= static_cast<uint32_t>(q[i]) << (8 * (i & 3));
+    return r;
+}
+__device__ __forceinline__ void store_codes(void* p, int at, int left, raw2_t r) {
+    uint8_t* q = static_cast<uint8_t*>(p) + at;
+    if (left >= 8) {
+        __builtin_nontemporal_store(r, reinterpret_cast<raw2_on1_t*>(q));
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < left) q[i] = static_cast<uint8_t>(r[i / 4] >> (8 * (i & 3)));
+}
+
+// ... and 8 bits.  Every lane of the wavefront takes part in store(), those without elements too.
+struct MomentsQ8 {
+    float m[8], v[8];
+    __device__ __forceinline__ void load(const Chunk& c, int at, int left) {
+        const raw2_t a = load_codes(c.M, at, left), b = load_codes(c.V, at, left);
+        const float sm = left > 0 ? c.mscale[at / kQBlock] : 0.f, sv = left > 0 ? c.vscale[at / kQBlock] : 0.f;
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+            const f32x2_t m0 = __builtin_amdgcn_cvt_pk_f32_fp8(a[w], false), m1 = __builtin_amdgcn_cvt_pk_f32_fp8(a[w], true);
+            const f32x2_t v0 = __builtin_amdgcn_cvt_pk_f32_bf8(b[w], false), v1 = __builtin_amdgcn_cvt_pk_f32_bf8(b[w], true);
+            m[4 * w] = m0.x * sm; m[4 * w + 1] = m0.y * sm; m[4 * w + 2] = m1.x * sm; m[4 * w + 3] = m1.y * sm;
+            v[4 * w] = v0.x * sv; v[4 * w + 1] = v0.y * sv; v[4 * w + 2] = v1.x * sv; v[4 * w + 3] = v1.y * sv;
+        }
+    }
+    __device__ __forceinline__ void store(const Chunk& c, int at, int left, uint32_t t) const {
+        const uint32_t em = CodeM::exponent(m), ev = CodeV::exponent(v);
+        const uint32_t j = static_cast<uint32_t>(at % kQBlock) * 0x9E3779B1u;
+        const raw2_t a = CodeM::codes(m, em, j + t * 0x6A09E667u), b = CodeV::codes(v, ev, j + t * 0xBB67AE85u);
+        if (left <= 0) return;
+        store_codes(c.M, at, left, a);
+        store_codes(c.V, at, left, b);
+        if (at % kQBlock == 0) {
+            c.mscale[at / kQBlock] = CodeM::scale(em);
+            c.vscale[at / kQBlock] = CodeV::scale(ev);
+        }
+    }
+};
+
+template <typename W, typename G, typename Moments>
+__global__ __launch_bounds__(kThreads) void adamw_kernel(StepArgs a) {
+    const Chunk c = a.chunks[blockIdx.x];
+    const AdamParams p = resolve(a.adam);
+    const uint32_t t = p.step_scalars ? static_cast<uint32_t>(p.step_scalars[3]) : a.t;
+    const float grad_scale = a.grad_scale ? *a.grad_scale : 1.0f;
+    if (grad_scale != grad_scale) return;
+    const int at = threadIdx.x * 8, left = c.elems - at;
+    Raw8<W> w;
+    Raw8<G> g;
+    W* pw = static_cast<W*>(c.W) + at;
+    const G* pg = static_cast<const G*>(c.G) + at;
+    if (left >= 8) {
+        w.load_once(pw);
+        g.load_once(pg);
+    } else {
+        w.load_some(pw, left);
+        g.load_some(pg, left);
+    }
+    Moments s;
+    s.load(c, at, left);
+    float out[8];
+    const float keep = 1.0f - p.lr * c.weight_decay;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        {
+#pragma clang fp contract(off)
+            const float x = g.get(i) * grad_scale;
+            const float m0 = p.b1 * s.m[i], m1 = p.one_minus_b1 * x;
+            const float v0 = p.b2 * s.v[i], v1 = p.one_minus_b2 * x;
+            s.m[i] = m0 + m1;
+            s.v[i] = v0 + v1 * x;
+        }
+        // hardware square root and reciprocal, as in adam_elem
+        const float step = p.lr * (s.m[i] * p.inv_c1) * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(s.v[i] * p.inv_c2) + p.eps);
+        out[i] = w.get(i) * keep - step;
+    }
+    s.store(c, at, left, t);
+    w.set(out);
+    if (left >= 8) w.store_once(pw);
+    else w.store_some(pw, left);
+}
+
+constexpr int kNormBlocks = 2048;
+
+template <typename G>
+__device__ __forceinline__ double squares(const Chunk& c) {
+    const int at = threadIdx.x * 8, left = c.elems - at;
+    Raw8<G> g;
+    if (left >= 8) g.load(static_cast<const G*>(c.G) + at);
+    else g.load_some(static_cast<const G*>(c.G) + at, left);
+    double s = 0.0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s += static_cast<double>(g.get(i)) * static_cast<double>(g.get(i));
+    return s;
+}
+
+__device__ __forceinline__ double block_sum(double s) {
+    __shared__ double part[kThreads / kWave];
+#pragma unroll
+    for (int o = kWave / 2; o > 0; o >>= 1) s += __shfl_xor(s, o, kWave);
+    if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = s;
+    __syncthreads();
+    return (part[0] + part[1]) + (part[2] + part[3]);
+}
+
+__global__ __launch_bounds__(kThreads) void grad_squares_kernel(const Chunk* __restrict__ chunks, int64_t count, double* part) {
+    double s = 0.0;
+    for (int64_t k = blockIdx.x; k < count; k += gridDim.x) {
+        const Chunk c = chunks[k];
+        s += c.gdt == GRASS_F32 ? squares<float>(c) : squares<uint16_t>(c);
+    }
+    s = block_sum(s);
+    if (threadIdx.x == 0) part[blockIdx.x] = s;
+}
+
+__global__ __launch_bounds__(kThreads) void grad_norm_kernel(const double* __restrict__ part, int count, float max_norm, float* out) {
+    double s = 0.0;
+    for (int k = threadIdx.x; k < count; k += kThreads) s += part[k];
+    s = block_sum(s);
+    if (threadIdx.x != 0) return;
+    const double norm = sqrt(s);
+    out[0] = static_cast<float>(norm);
+    const double factor = norm > static_cast<double>(max_norm) ? static_cast<double>(max_norm) / norm : 1.0;
+    out[1] = s <= 1.7976931348623157e308 ? static_cast<float>(factor) : __uint_as_float(0x7FC00000u);
+}
+
+int64_t chunks_in(const grass_adamw_layout& layout) {
+    int64_t n = 0;
+    for (int i = 0; i < GRASS_ADAMW_GROUPS; ++i) n += layout.chunks[i];
+    return n;
+}
+
+int norm_blocks(const grass_adamw_layout& layout) {
+    const int64_t n = chunks_in(layout);
+    return static_cast<int>(n < kNormBlocks ? n : kNormBlocks);
+}
+
+}  // namespace
+
+void adamw_count(int count, const grass_adamw_tensor* tensors, grass_adamw_layout* layout) {
+    *layout = grass_adamw_layout{};
+    for (int i = 0; i < count; ++i) {
+        const Pieces p = pieces_of(tensors[i]);
+        layout->chunks[group_of(tensors[i])] += p.count * ((p.elems + kChunk - 1) / kChunk);
+    }
+}
+
+size_t adamw_plan_bytes(const grass_adamw_layout& layout) { return static_cast<size_t>(chunks_in(layout)) * sizeof(Chunk); }
+
+void adamw_lay_out(int count, const grass_adamw_tensor* tensors, const grass_adamw_layout& layout, void* plan) {
+    Chunk* next[GRASS_ADAMW_GROUPS];
+    Chunk* at = static_cast<Chunk*>(plan);
+    for (int i = 0; i < GRASS_ADAMW_GROUPS; ++i) {
+        next[i] = at;
+        at += layout.chunks[i];
+    }
+    for (int i = 0; i < count; ++i) {
+        const grass_adamw_tensor& a = tensors[i];
+        const Pieces p = pieces_of(a);
+        Chunk*& out = next[group_of(a)];
+        const int64_t wsize = a.wdt == GRASS_F32 ? 4 : 2, gsize = a.gdt == GRASS_F32 ? 4 : 2;
+        const bool q8 = a.moments == GRASS_MOMENTS_Q8;
+        for (int64_t r = 0; r < p.count; ++r)
+            for (int64_t e = 0; e < p.elems; e += kChunk) {
+                Chunk c{};
+                c.G = static_cast<const char*>(a.G) + (r * a.ldg + e) * gsize;
+                c.elems = static_cast<int32_t>(p.elems - e < kChunk ? p.elems - e : kChunk);
+                c.gdt = a.gdt;
+                if (a.W) {
+                    const int64_t s = r * a.cols + e;
+                    c.W = static_cast<char*>(a.W) + (r * a.ldw + e) * wsize;
+                    c.M = static_cast<char*>(a.M) + s * (q8 ? 1 : 4);
+                    c.V = static_cast<char*>(a.V) + s * (q8 ? 1 : 4);
+                    c.mscale = q8 ? a.mscale + s / kQBlock : nullptr;
+                    c.vscale = q8 ? a.vscale + s / kQBlock : nullptr;
+                    c.weight_decay = a.weight_decay;
+                }
+                *out++ = c;
+            }
+    }
+}
+
+bool adamw_steps(const grass_adamw_layout& layout) {
+    for (int i = kStepGroups; i < GRASS_ADAMW_GROUPS; ++i)
+        if (layout.chunks[i] != 0) return false;
+    return true;
+}
+
+void adamw_step_scalars(float lr, float b1, float b2, int64_t t, float out[4]) {
+    adam_step_scalars(lr, b1, b2, t, out);
+    out[3] = static_cast<float>(t % (1 << 24));
+}
+
+grass_status launch_adamw(const void* plan, const grass_adamw_layout& layout, float lr, float b1, float b2,
+                          float eps, int64_t t, const float* step_scalars, const float* grad_scale, hipStream_t s) {
+    if (chunks_in(layout) == 0) return GRASS_OK;
+    StepArgs a{static_cast<const Chunk*>(plan), make_params(lr, b1, b2, eps, t, step_scalars),
+               static_cast<uint32_t>(t % (1 << 24)), grad_scale};
+    for (int i = 0; i < kStepGroups; ++i) {
+        // a grid has fewer than 2^32 threads
+        for (int64_t left = layout.chunks[i]; left > 0;) {
+            const int64_t now = left < (int64_t{1} << 23) ? left : int64_t{1} << 23;
+            const unsigned grid = static_cast<unsigned>(now);
+            switch (i) {
+                case 0: adamw_kernel<float, float, MomentsF32><<<grid, kThreads, 0, s>>>(a); break;
+                case 1: adamw_kernel<float, float, MomentsQ8><<<grid, kThreads, 0, s>>>(a); break;
+                case 2: adamw_kernel<float, uint16_t, MomentsF32><<<grid, kThreads, 0, s>>>(a); break;
+                case 3: adamw_kernel<float, uint16_t, MomentsQ8><<<grid, kThreads, 0, s>>>(a); break;
+                case 4: adamw_kernel<uint16_t, float, MomentsF32><<<grid, kThreads, 0, s>>>(a); break;
+                case 5: adamw_kernel<uint16_t, float, MomentsQ8><<<grid, kThreads, 0, s>>>(a); break;
+                case 6: adamw_kernel<uint16_t, uint16_t, MomentsF32><<<grid, kThreads, 0, s>>>(a); break;
+                case 7: adamw_kernel<uint16_t, uint16_t, MomentsQ8><<<grid, kThreads, 0, s>>>(a); break;
+            }
+            a.chunks += now;
+            left -= now;
+        }
+    }
+    return launch_status();
+}
+
+size_t grad_norm_workspace_bytes(const grass_adamw_layout& layout) {
+    return static_cast<size_t>(norm_blocks(layout)) * sizeof(double);
+}
+
+grass_status launch_grad_norm(const void* plan, const grass_adamw_layout& layout, float max_norm, float* out,
+                              void* ws, hipStream_t s) {
+    const int blocks = norm_blocks(layout);
+    double* part = static_cast<double*>(ws);
+    if (blocks > 0)
+        grad_squares_kernel<<<static_cast<unsigned>(blocks), kThreads, 0, s>>>(static_cast<const Chunk*>(plan),
+                                                                               chunks_in(layout), part);
+    grad_norm_kernel<<<1, kThreads, 0, s>>>(part, blocks, max_norm, out);
+    return launch_status();
+}
+
+}  // namespace grass

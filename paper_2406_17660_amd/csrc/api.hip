@@ -477,6 +477,143 @@ grass_status grass_gather_rows(const void* G, grass_dtype gdt, int64_t m, int64_
     return launch_gather_rows(G, gdt, n, ldg, idx, rho, r, out, ldo, as_stream(stream));
 }
 
+static grass_status check_norm(grass_norm kind, grass_dtype dt, grass_dtype gdt, int64_t T, int64_t n) {
+    if (T < 0 || n < 1 || !small(T) || !small(n)) return GRASS_ERR_SHAPE;
+    if (kind != GRASS_NORM_LAYER && kind != GRASS_NORM_RMS) return GRASS_ERR_DTYPE;
+    return dtype_ok(dt) && dtype_ok(gdt) ? GRASS_OK : GRASS_ERR_DTYPE;
+}
+
+grass_status grass_norm_forward(grass_norm kind, const void* X, int64_t ldx, const void* R,
+                                int64_t ldr, grass_dtype dt, int64_t T, int64_t n, const void* gain,
+                                const void* bias, grass_dtype gdt, float eps, void* H, int64_t ldh,
+                                void* Y, int64_t ldy, float* mean, float* rstd, void* stream) {
+    const grass_status st = check_norm(kind, dt, gdt, T, n);
+    if (st != GRASS_OK) return st;
+    if (ldx < n || ldy < n || (R && (ldr < n || ldh < n)) || !(eps >= 0.f)) return GRASS_ERR_SHAPE;
+    if (!present(X, T) || !present(Y, T) || (R && !present(H, T))) return GRASS_ERR_NULL;
+    return launch_norm_forward(kind, X, ldx, R, ldr, dt, T, n, gain, bias, gdt, eps, R ? H : nullptr, ldh, Y, ldy,
+                               mean, rstd, as_stream(stream));
+}
+
+size_t grass_norm_backward_workspace(int64_t T, int64_t n, grass_dtype dt) {
+    if (T < 0 || n < 1 || !small(T) || !small(n) || !dtype_ok(dt)) return 0;
+    return norm_backward_workspace_bytes(T, n);
+}
+
+grass_status grass_norm_backward(grass_norm kind, const void* dY, int64_t lddy, const void* H,
+                                 int64_t ldh, const void* dR, int64_t lddr, grass_dtype dt, int64_t T,
+                                 int64_t n, const void* gain, grass_dtype gdt, const float* mean,
+                                 const float* rstd, void* dX, int64_t lddx, float* dgain,
+                                 float* dbias, void* ws, size_t ws_bytes, void* stream) {
+    const grass_status st = check_norm(kind, dt, gdt, T, n);
+    if (st != GRASS_OK) return st;
+    if (lddy < n || ldh < n || (dR && lddr < n) || lddx < n) return GRASS_ERR_SHAPE;
+    if (!present(dY, T) || !present(H, T) || !present(rstd, T) || !present(dX, T) ||
+        (kind == GRASS_NORM_LAYER && !present(mean, T)))
+        return GRASS_ERR_NULL;
+    const size_t need = dgain || dbias ? norm_backward_workspace_bytes(T, n) : 0;
+    if (need > 0 && (!ws || ws_bytes < need)) return GRASS_ERR_WORKSPACE;
+    return launch_norm_backward(kind, dY, lddy, H, ldh, dR, lddr, dt, T, n, gain, gdt, mean, rstd, dX, lddx, dgain,
+                                dbias, ws, as_stream(stream));
+}
+
+static grass_status check_adamw_tensors(int count, const grass_adamw_tensor* tensors) {
+    if (count < 0) return GRASS_ERR_SHAPE;
+    if (count > 0 && !tensors) return GRASS_ERR_NULL;
+    for (int i = 0; i < count; ++i) {
+        const grass_adamw_tensor& a = tensors[i];
+        if (a.rows < 0 || a.cols < 0 || !small(a.rows) || !small(a.cols) || a.ldg < a.cols) return GRASS_ERR_SHAPE;
+        const int64_t elems = a.rows * a.cols;
+        if (!present(a.G, elems)) return GRASS_ERR_NULL;
+        if (!dtype_ok(a.gdt)) return GRASS_ERR_DTYPE;
+        if (!aligned_to(a.G, a.gdt == GRASS_F32 ? 4 : 2)) return GRASS_ERR_SHAPE;
+        if (!a.W && !a.M && !a.V) continue;  // gradients alone
+        if (a.ldw < a.cols) return GRASS_ERR_SHAPE;
+        if (!present(a.W, elems) || !present(a.M, elems) || !present(a.V, elems)) return GRASS_ERR_NULL;
+        if (!dtype_ok(a.wdt) || (a.moments != GRASS_MOMENTS_F32 && a.moments != GRASS_MOMENTS_Q8))
+            return GRASS_ERR_DTYPE;
+        if (!aligned_to(a.W, a.wdt == GRASS_F32 ? 4 : 2)) return GRASS_ERR_SHAPE;
+        if (a.moments == GRASS_MOMENTS_F32) {
+            if (!aligned_to(a.M, 4) || !aligned_to(a.V, 4)) return GRASS_ERR_SHAPE;
+            continue;
+        }
+        if (!present(a.mscale, elems) || !present(a.vscale, elems)) return GRASS_ERR_NULL;
+        if (!aligned_to(a.mscale, 4) || !aligned_to(a.vscale, 4)) return GRASS_ERR_SHAPE;
+        if (a.rows > 1 && (a.ldw != a.cols || a.ldg != a.cols) && a.cols % 128 != 0) return GRASS_ERR_SHAPE;
+    }
+    return GRASS_OK;
+}
+
+size_t grass_adamw_plan_bytes(int count, const grass_adamw_tensor* tensors) {
+    if (check_adamw_tensors(count, tensors) != GRASS_OK) return 0;
+    grass_adamw_layout layout;
+    adamw_count(count, tensors, &layout);
+    return adamw_plan_bytes(layout);
+}
+
+grass_status grass_adamw_plan(int count, const grass_adamw_tensor* tensors, void* plan,
+                              size_t plan_bytes, grass_adamw_layout* layout) {
+    const grass_status st = check_adamw_tensors(count, tensors);
+    if (st != GRASS_OK) return st;
+    if (!layout) return GRASS_ERR_NULL;
+    grass_adamw_layout found;
+    adamw_count(count, tensors, &found);
+    if (!present(plan, static_cast<int64_t>(adamw_plan_bytes(found)))) return GRASS_ERR_NULL;
+    if (plan_bytes < adamw_plan_bytes(found)) return GRASS_ERR_WORKSPACE;
+    *layout = found;
+    adamw_lay_out(count, tensors, found, plan);
+    return GRASS_OK;
+}
+
+// A layout that grass_adamw_plan can have written, and the plan beside it.
+static grass_status check_adamw_plan(const void* plan, const grass_adamw_layout* layout) {
+    if (!layout) return GRASS_ERR_NULL;
+    int64_t chunks = 0;
+    for (int i = 0; i < GRASS_ADAMW_GROUPS; ++i) {
+        if (layout->chunks[i] < 0 || !small(layout->chunks[i])) return GRASS_ERR_SHAPE;
+        chunks += layout->chunks[i];
+    }
+    if (!present(plan, chunks)) return GRASS_ERR_NULL;
+    return aligned_to(plan, 16) ? GRASS_OK : GRASS_ERR_SHAPE;
+}
+
+grass_status grass_adamw_step(const void* plan, const grass_adamw_layout* layout, float lr,
+                              float beta1, float beta2, float eps, int64_t t,
+                              const float* step_scalars, const float* grad_scale, void* stream) {
+    const grass_status st = check_adamw_plan(plan, layout);
+    if (st != GRASS_OK) return st;
+    if ((!step_scalars && t < 1) || !(beta1 >= 0.f && beta1 < 1.f) || !(beta2 >= 0.f && beta2 < 1.f))
+        return GRASS_ERR_SHAPE;
+    if (!adamw_steps(*layout)) return GRASS_ERR_SHAPE;
+    return launch_adamw(plan, *layout, lr, beta1, beta2, eps, step_scalars ? 1 : t, step_scalars, grad_scale,
+                        as_stream(stream));
+}
+
+grass_status grass_adamw_step_scalars(float lr, float beta1, float beta2, int64_t t,
+                                      float* scalars) {
+    if (!scalars) return GRASS_ERR_NULL;
+    if (t < 1 || !(beta1 >= 0.f && beta1 < 1.f) || !(beta2 >= 0.f && beta2 < 1.f))
+        return GRASS_ERR_SHAPE;
+    adamw_step_scalars(lr, beta1, beta2, t, scalars);
+    return GRASS_OK;
+}
+
+size_t grass_grad_norm_workspace(const grass_adamw_layout* layout) {
+    if (check_adamw_plan(reinterpret_cast<const void*>(16), layout) != GRASS_OK) return 0;
+    return grad_norm_workspace_bytes(*layout);
+}
+
+grass_status grass_grad_norm(const void* plan, const grass_adamw_layout* layout, float max_norm,
+                             float* out, void* ws, size_t ws_bytes, void* stream) {
+    const grass_status st = check_adamw_plan(plan, layout);
+    if (st != GRASS_OK) return st;
+    if (!out) return GRASS_ERR_NULL;
+    if (!(max_norm >= 0.f)) return GRASS_ERR_SHAPE;
+    const size_t need = grad_norm_workspace_bytes(*layout);
+    if (need > 0 && (!ws || ws_bytes < need || !aligned_to(ws, 8))) return GRASS_ERR_WORKSPACE;
+    return launch_grad_norm(plan, *layout, max_norm, out, ws, as_stream(stream));
+}
+
 grass_status grass_set_test_option(grass_test_option option, int value) {
     const int which = static_cast<int>(option);
     if (which < 0 || which >= kNumTestOptions) return GRASS_ERR_DTYPE;

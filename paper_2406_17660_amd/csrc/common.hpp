@@ -289,4 +289,28 @@ grass_status launch_grad_row_stats(const void* dY, grass_dy_layout layout, int64
                                    int64_t n, float* sumsq, void* ws, size_t ws_bytes,
                                    hipStream_t s);
 
+// Layer norm and RMS norm.
+grass_status launch_norm_forward(grass_norm kind, const void* X, int64_t ldx, const void* R, int64_t ldr,
+                                 grass_dtype dt, int64_t T, int64_t n, const void* gain, const void* bias,
+                                 grass_dtype gdt, float eps, void* H, int64_t ldh, void* Y, int64_t ldy,
+                                 float* mean, float* rstd, hipStream_t s);
+size_t norm_backward_workspace_bytes(int64_t T, int64_t n);
+grass_status launch_norm_backward(grass_norm kind, const void* dY, int64_t lddy, const void* H, int64_t ldh,
+                                  const void* dR, int64_t lddr, grass_dtype dt, int64_t T, int64_t n,
+                                  const void* gain, grass_dtype gdt, const float* mean, const float* rstd,
+                                  void* dX, int64_t lddx, float* dgain, float* dbias, void* ws, hipStream_t s);
+
+// AdamW over many tensors and the norm of their gradients.  The tensors have been checked; the
+// number of chunks that a plan of them has, by group, and the plan itself.
+void adamw_count(int count, const grass_adamw_tensor* tensors, grass_adamw_layout* layout);
+size_t adamw_plan_bytes(const grass_adamw_layout& layout);
+void adamw_lay_out(int count, const grass_adamw_tensor* tensors, const grass_adamw_layout& layout, void* plan);
+bool adamw_steps(const grass_adamw_layout& layout);  // no chunks that name only gradients
+grass_status launch_adamw(const void* plan, const grass_adamw_layout& layout, float lr, float b1, float b2,
+                          float eps, int64_t t, const float* step_scalars, const float* grad_scale, hipStream_t s);
+void adamw_step_scalars(float lr, float b1, float b2, int64_t t, float out[4]);
+size_t grad_norm_workspace_bytes(const grass_adamw_layout& layout);
+grass_status launch_grad_norm(const void* plan, const grass_adamw_layout& layout, float max_norm, float* out,
+                              void* ws, hipStream_t s);
+
 }  // namespace grass

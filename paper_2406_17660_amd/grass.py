@@ -22,6 +22,9 @@ DY_TxM, DY_MxT = 0, 1
 TEST_GEMM_TILE, TEST_FUSED_STATS, TEST_PACK_MXT, TEST_NO_PAIRS, TEST_MAX_K_SLICES = 0, 1, 2, 3, 4
 TEST_NO_NARROW_GATHER, TEST_RUN_TILE, TEST_UNALIGNED_X = 5, 6, 7
 CALL_CGRAD, CALL_STEP, CALL_DENSE = range(3)
+NORM_LAYER, NORM_RMS = 0, 1
+MOMENTS_F32, MOMENTS_Q8 = 0, 1
+MOMENTS_BLOCK = 128  # elements of an 8-bit moment that share a scale
 (KERNEL_NONE, KERNEL_128_STAGED, KERNEL_128, KERNEL_128_256, KERNEL_256, KERNEL_256_ROWS, KERNEL_256_UNALIGNED,
  KERNEL_256_UNALIGNED_X, KERNEL_NARROW, KERNEL_F32, KERNEL_F32_SPLIT_64, KERNEL_F32_SPLIT_128,
  KERNEL_F32_SHORT, KERNEL_256_UNALIGNED_DY) = range(14)
@@ -39,6 +42,9 @@ EXPORTS = [
     "grass_adam_step_scalars", "grass_adam_scatter_replayable",
     "grass_step_group_workspace", "grass_step_group", "grass_step_group_timed",
     "grass_step_cols_workspace", "grass_step_cols",
+    "grass_norm_forward", "grass_norm_backward_workspace", "grass_norm_backward",
+    "grass_adamw_plan_bytes", "grass_adamw_plan", "grass_adamw_step", "grass_adamw_step_scalars",
+    "grass_grad_norm_workspace", "grass_grad_norm",
 ]
 
 _lib = None
@@ -49,6 +55,19 @@ class StepLayer(C.Structure):
     _fields_ = [("dY", C.c_void_p), ("ldy", C.c_int64), ("m", C.c_int64), ("r", C.c_int64),
                 ("idx", C.c_void_p), ("rho", C.c_void_p), ("GC", C.c_void_p), ("ldgc", C.c_int64),
                 ("M", C.c_void_p), ("V", C.c_void_p), ("W", C.c_void_p), ("ldw", C.c_int64)]
+
+
+class AdamWTensor(C.Structure):
+    """grass_adamw_tensor of include/grass.h."""
+    _fields_ = [("W", C.c_void_p), ("G", C.c_void_p), ("M", C.c_void_p), ("V", C.c_void_p),
+                ("mscale", C.c_void_p), ("vscale", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64),
+                ("ldw", C.c_int64), ("ldg", C.c_int64), ("wdt", C.c_int), ("gdt", C.c_int),
+                ("moments", C.c_int), ("weight_decay", C.c_float)]
+
+
+class AdamWLayout(C.Structure):
+    """grass_adamw_layout of include/grass.h."""
+    _fields_ = [("chunks", C.c_int64 * 10)]
 
 
 class GrassError(RuntimeError):
@@ -120,12 +139,29 @@ def lib():
     L.grass_cgrad_group_workspace.restype = sz
     L.grass_compressed_grad_group.argtypes = [i32, vp, i32, vp, vp, i64, i32, i64, vp, i64, vp,
                                               vp, vp, vp, vp, vp, sz, vp]
+    L.grass_norm_forward.argtypes = [i32, vp, i64, vp, i64, i32, i64, i64, vp, vp, i32, f32, vp, i64,
+                                     vp, i64, vp, vp, vp]
+    L.grass_norm_backward_workspace.argtypes = [i64, i64, i32]
+    L.grass_norm_backward_workspace.restype = sz
+    L.grass_norm_backward.argtypes = [i32, vp, i64, vp, i64, vp, i64, i32, i64, i64, vp, i32, vp, vp,
+                                      vp, i64, vp, vp, vp, sz, vp]
+    layout = C.POINTER(AdamWLayout)
+    L.grass_adamw_plan_bytes.argtypes = [i32, vp]
+    L.grass_adamw_plan_bytes.restype = sz
+    L.grass_adamw_plan.argtypes = [i32, vp, vp, sz, layout]
+    L.grass_adamw_step.argtypes = [vp, layout, f32, f32, f32, f32, i64, vp, vp, vp]
+    L.grass_adamw_step_scalars.argtypes = [f32, f32, f32, i64, C.POINTER(C.c_float)]
+    L.grass_grad_norm_workspace.argtypes = [layout]
+    L.grass_grad_norm_workspace.restype = sz
+    L.grass_grad_norm.argtypes = [vp, layout, f32, vp, vp, sz, vp]
     for name in EXPORTS:
         if name not in ("grass_status_string", "grass_select_workspace", "grass_cgrad_workspace",
                         "grass_select_static_capacity",
                         "grass_dense_workspace", "grass_grad_row_stats_workspace",
                         "grass_cgrad_group_workspace", "grass_step_group_workspace",
-                        "grass_step_cols_workspace", "grass_test_least_workspace"):
+                        "grass_step_cols_workspace", "grass_test_least_workspace",
+                        "grass_norm_backward_workspace", "grass_adamw_plan_bytes",
+                        "grass_grad_norm_workspace"):
             getattr(L, name).restype = i32
     L.grass_test_product_us.argtypes = [i32, i32, i64, i64]
     L.grass_test_product_us.restype = C.c_double
@@ -537,6 +573,157 @@ def gather_rows(G, idx, rho, out):
     _check(lib().grass_gather_rows(pG, _dtype(G), m, n, ldg, _vec(idx, torch.int32),
                                    _vec(rho, torch.float32), r, pO, ldo, _stream()),
            "grass_gather_rows")
+    return out
+
+
+def _norm_vec(t, n, dtype=None):
+    """Address of a vector of n values, or None."""
+    if t is None:
+        return None
+    assert t.is_cuda and t.shape == (n,) and t.is_contiguous() and (dtype is None or t.dtype == dtype)
+    return t.data_ptr()
+
+
+def _norm_mat(t, T, n, dtype):
+    """(address, leading dimension) of a T x n matrix, or (None, n)."""
+    if t is None:
+        return None, n
+    p, rows, cols, ld = _mat(t)
+    assert (rows, cols) == (T, n) and t.dtype == dtype
+    return p, ld
+
+
+def _gain_dtype(gain, bias):
+    given = [t for t in (gain, bias) if t is not None]
+    assert len({t.dtype for t in given}) <= 1, "gain and bias have one dtype"
+    return _dtype(given[0]) if given else F32
+
+
+def norm_forward(X, gain, bias, eps, Y, kind=NORM_LAYER, R=None, H=None, mean=None, rstd=None):
+    """Layer norm or RMS norm (kind) of the rows of X, or of X + R, which H then receives; mean and
+    rstd: T floats for the backward pass, or None."""
+    pX, T, n, ldx = _mat(X)
+    pR, ldr = _norm_mat(R, T, n, X.dtype)
+    pH, ldh = _norm_mat(H, T, n, X.dtype)
+    pY, ldy = _norm_mat(Y, T, n, X.dtype)
+    _check(lib().grass_norm_forward(kind, pX, ldx, pR, ldr, _dtype(X), T, n, _norm_vec(gain, n), _norm_vec(bias, n),
+                                    _gain_dtype(gain, bias), eps, pH, ldh, pY, ldy, _norm_vec(mean, T, torch.float32),
+                                    _norm_vec(rstd, T, torch.float32), _stream()), "grass_norm_forward")
+    return Y
+
+
+def norm_backward_workspace(T, n, dtype) -> int:
+    return int(lib().grass_norm_backward_workspace(T, n, dtype))
+
+
+def norm_backward(dY, H, gain, mean, rstd, dX, dgain, dbias, ws, kind=NORM_LAYER, dR=None):
+    """Backward pass of norm_forward: dX (plus dR where given), dgain and dbias (fp32, or None) from the
+    rows H that were normed and the statistics that the forward pass kept."""
+    pY, T, n, lddy = _mat(dY)
+    pH, ldh = _norm_mat(H, T, n, dY.dtype)
+    pR, lddr = _norm_mat(dR, T, n, dY.dtype)
+    pX, lddx = _norm_mat(dX, T, n, dY.dtype)
+    wp, wb = _ws(ws)
+    _check(lib().grass_norm_backward(kind, pY, lddy, pH, ldh, pR, lddr, _dtype(dY), T, n, _norm_vec(gain, n),
+                                     _gain_dtype(gain, None), _norm_vec(mean, T, torch.float32),
+                                     _norm_vec(rstd, T, torch.float32), pX, lddx, _norm_vec(dgain, n, torch.float32),
+                                     _norm_vec(dbias, n, torch.float32), wp, wb, _stream()), "grass_norm_backward")
+    return dX
+
+
+_MOMENTS = {torch.float32: (MOMENTS_F32, torch.float32), torch.float8_e4m3fn: (MOMENTS_Q8, torch.float8_e5m2)}
+
+
+class AdamWPlan:
+    """Tensors laid out for grass_adamw_step and grass_grad_norm: the plan in device memory, its
+    layout, and the tensors (held, since the plan names their addresses)."""
+
+    def __init__(self, plan, layout, tensors):
+        self.plan, self.layout, self.tensors = plan, layout, tensors
+
+
+def _rows(t):
+    """(address, rows, cols, leading dimension) of a tensor as AdamW sees it: anything contiguous, or
+    a 2-D tensor with contiguous rows."""
+    assert t.is_cuda
+    if t.dim() == 2 and not t.is_contiguous():
+        return _mat(t)
+    assert t.is_contiguous(), "contiguous tensors, or matrices with contiguous rows"
+    n = t.numel()
+    if t.dim() == 2 and n > 0:
+        return t.data_ptr(), t.shape[0], t.shape[1], t.shape[1]
+    return t.data_ptr(), min(n, 1), n, n
+
+
+def adamw_plan(Ws, Gs, Ms, Vs, weight_decay=0.0, Mscales=None, Vscales=None):
+    """A plan over lists of weights, gradients and moments (fp32, or float8_e4m3fn M and float8_e5m2 V with
+    the blocks' scales in Mscales and Vscales); weight_decay: one value or one per tensor.  Ws, Ms
+    and Vs None: a plan of gradients for grad_norm alone."""
+    count = len(Gs)
+    tensors = (AdamWTensor * max(count, 1))()
+    decay = weight_decay if isinstance(weight_decay, (list, tuple)) else [weight_decay] * count
+    alone = Ws is None
+    assert len(decay) == count and (alone or len(Ws) == len(Ms) == len(Vs) == count)
+    for i, (a, G) in enumerate(zip(tensors, Gs)):
+        a.G, a.rows, a.cols, a.ldg = _rows(G)
+        a.gdt, a.weight_decay = _dtype(G), decay[i]
+        if alone:
+            continue
+        W, M, V = Ws[i], Ms[i], Vs[i]
+        assert W.shape == G.shape and M.numel() == V.numel() == G.numel(), "shapes differ"
+        a.W, rows, cols, a.ldw = _rows(W)
+        assert (rows, cols) == (a.rows, a.cols)
+        a.wdt = _dtype(W)
+        if M.dtype not in _MOMENTS or V.dtype != _MOMENTS[M.dtype][1]:
+            raise TypeError(f"unsupported moments {M.dtype}, {V.dtype}")
+        for t in (M, V):
+            assert t.is_cuda and t.is_contiguous()
+        a.M, a.V, a.moments = M.data_ptr(), V.data_ptr(), _MOMENTS[M.dtype][0]
+        if a.moments == MOMENTS_Q8:
+            for t in (Mscales[i], Vscales[i]):
+                assert t.shape == (moment_blocks(W.numel()),)
+            a.mscale, a.vscale = _vec(Mscales[i], torch.float32), _vec(Vscales[i], torch.float32)
+    layout = AdamWLayout()
+    host = torch.empty(int(lib().grass_adamw_plan_bytes(count, tensors)), dtype=torch.uint8)
+    _check(lib().grass_adamw_plan(count, tensors, host.data_ptr(), host.nbytes, C.byref(layout)), "grass_adamw_plan")
+    device = Gs[0].device if count else "cuda"
+    return AdamWPlan(host.to(device), layout, (Ws, Gs, Ms, Vs, Mscales, Vscales))
+
+
+def moment_blocks(elems: int) -> int:
+    """Scales that an 8-bit moment of so many elements has."""
+    return (elems + MOMENTS_BLOCK - 1) // MOMENTS_BLOCK
+
+
+def adamw_step(plan, lr, beta1, beta2, eps, t, grad_scale=None, step_scalars=None):
+    """One AdamW step of every tensor of the plan; grad_scale: a device float that the gradients are
+    multiplied by (NaN: the step changes nothing); step_scalars: the 4 floats of
+    adamw_step_scalars on the device, for captured steps."""
+    for a, least in ((grad_scale, 1), (step_scalars, 4)):
+        assert a is None or (a.is_cuda and a.dtype == torch.float32 and a.numel() >= least and a.is_contiguous())
+    _check(lib().grass_adamw_step(plan.plan.data_ptr(), C.byref(plan.layout), lr, beta1, beta2, eps, t,
+                                  None if step_scalars is None else step_scalars.data_ptr(),
+                                  None if grad_scale is None else grad_scale.data_ptr(), _stream()), "grass_adamw_step")
+
+
+def adamw_step_scalars(lr, beta1, beta2, t):
+    """(lr, 1/(1-beta1^t), 1/(1-beta2^t), t modulo 2^24) as the float32 values that a step reads."""
+    out = (C.c_float * 4)()
+    _check(lib().grass_adamw_step_scalars(lr, beta1, beta2, t, out), "grass_adamw_step_scalars")
+    return [out[0], out[1], out[2], out[3]]
+
+
+def grad_norm_workspace(plan) -> int:
+    return int(lib().grass_grad_norm_workspace(C.byref(plan.layout)))
+
+
+def grad_norm(plan, max_norm, out, ws):
+    """out[0]: the norm of all gradients of the plan, out[1]: the factor that clips it to max_norm (a
+    grad_scale of adamw_step; NaN where the norm is not finite)."""
+    assert out.is_cuda and out.dtype == torch.float32 and out.numel() >= 2 and out.is_contiguous()
+    wp, wb = _ws(ws)
+    _check(lib().grass_grad_norm(plan.plan.data_ptr(), C.byref(plan.layout), max_norm, out.data_ptr(), wp, wb,
+                                 _stream()), "grass_grad_norm")
     return out
 
 

@@ -1,0 +1,73 @@
+"""The 8-bit moments as the tests' CPU code forms them: against torch's own e4m3 and e5m2 types, the bounds
+of the rounding, and what the thresholds are for."""
+import numpy as np
+import pytest
+import torch
+
+import adamw_ref
+
+TYPES = {"M": torch.float8_e4m3fn, "V": torch.float8_e5m2}
+
+
+@pytest.mark.parametrize("kind", ["M", "V"])
+def test_every_code_is_the_types_value(kind):
+    code = np.arange(256, dtype=np.uint8)
+    want = torch.from_numpy(code).view(TYPES[kind]).float().numpy()
+    got = adamw_ref.decode(code, np.ones(2, np.float32), kind)
+    assert np.array_equal(got, want, equal_nan=True)
+
+
+@pytest.mark.parametrize("kind", ["M", "V"])
+@pytest.mark.parametrize("t", [1, 2, 1000, (1 << 24) + 5])
+def test_codes_are_a_neighbour_of_the_value(kind, t):
+    rng = np.random.default_rng(t)
+    man, top, low, _ = adamw_ref.KIND[kind]
+    x = (rng.normal(size=1000) * np.exp(rng.normal(size=1000) * 4)).astype(np.float32)
+    x = np.abs(x) if kind == "V" else x
+    x[:7] = [0, 1e-45, -1e-45 if kind == "M" else 1e-45, 1e-30, 3e-38, 2e-20, 1]
+    code, scale = adamw_ref.encode(x, t, kind)
+    back = adamw_ref.decode(code, scale, kind).astype(np.float64)
+    s = np.repeat(scale.astype(np.float64), 128)[:x.size]
+    step = np.maximum(2.0 ** (np.floor(np.log2(np.maximum(np.abs(x) / s, 1e-300))) - man), 2.0 ** (low - man))
+    assert (np.abs(back - x) <= step * s).all()
+    assert np.isfinite(back).all() and (back[x == 0] == 0).all()
+
+
+@pytest.mark.parametrize("kind", ["M", "V"])
+def test_the_thresholds_lose_nothing_on_average(kind):
+    """A value between two codes is on average itself: over 4096 steps to a thousandth of a step (a random
+    threshold would leave 1 / 128), within a block of 128 at one step to a tenth."""
+    man = adamw_ref.KIND[kind][0]
+    x = np.full(128, np.float32(1.0 + 0.3 / 2 ** man))
+    x[0] = 1.9
+    got = np.mean([adamw_ref.decode(*adamw_ref.encode(x, t, kind), kind)[5] for t in range(1, 4097)])
+    assert abs(got - x[5]) < 2.0 ** -man / 1000
+    one = adamw_ref.decode(*adamw_ref.encode(x, 77, kind), kind)[1:]
+    assert abs(one.mean() - x[5]) < 2.0 ** -man / 10
+
+
+def test_second_moments_follow_small_changes():
+    """With b2 = 0.999 a constant gradient's second moment ends at its square, where rounding to the
+    nearest code would leave it as soon as a step adds less than half a code's distance: an eighth."""
+    g = np.full(128, np.float32(0.01))
+    code, scale = np.zeros(128, np.uint8), np.ones(1, np.float32)
+    seen = []
+    for t in range(1, 6001):
+        v = adamw_ref.decode(code, scale, "V")
+        _, v = adamw_ref.moments(g, 1.0, v, v, 0.9, 0.999)
+        code, scale = adamw_ref.encode(v, t, "V")
+        if t > 5000:
+            seen.append(adamw_ref.decode(code, scale, "V").mean())
+    assert abs(np.mean(seen) / (g[0] ** 2) - 1) < 0.05
+
+
+def test_infinities_and_nan_are_stored_as_nan_and_alone():
+    x = np.linspace(0.5, 1.5, 130).astype(np.float32)
+    want = adamw_ref.encode(x, 9, "M")
+    y = x.copy()
+    y[3], y[70] = np.inf, np.nan
+    code, scale = adamw_ref.encode(y, 9, "M")
+    keep = np.ones(130, bool)
+    keep[[3, 70]] = False
+    assert np.array_equal(code[keep], want[0][keep]) and np.array_equal(scale, want[1])
+    assert np.isnan(adamw_ref.decode(code, scale, "M")[[3, 70]]).all()

@@ -1,0 +1,270 @@
+"""grass_adamw_step and grass_grad_norm against CPU code of the same formulas.
+
+The moments have to be equal bit for bit: fp32 products and sums in a stated order, and codes that follow
+from them.  Weights: an fp32 result within 24 half steps of fp32 of the magnitudes that enter it
+(hardware square root and reciprocal, a step each, the products, and the fp32 bias corrections), rounded once to
+its type: half a step, finfo.eps / 2."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import adamw_ref
+from gpu_util import DEV, to_f64
+from paper_2406_17660_amd import grass
+
+pytestmark = pytest.mark.gpu
+LR, B1, B2, EPS = 1e-3, 0.9, 0.999, 1e-8
+FP32 = 24 * 2.0 ** -24
+F32, BF16 = torch.float32, torch.bfloat16
+SIZES = [1, 2, 7, 8, 9, 127, 128, 129, 255, 1000, 2047, 2048, 2049, 4096, 5003]
+
+
+def draw(n, seed, dtype, scale=1.0):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return (torch.randn(n, generator=g, device=DEV) * scale).to(dtype)
+
+
+class Tensor:
+    """One parameter with its gradient and moments, `offset` elements into its buffers, and CPU copies."""
+
+    def __init__(self, n, seed, wdt, gdt, q8, offset=0, decay=0.0, zero=False):
+        self.n, self.q8, self.decay = n, q8, decay
+
+        def buffer(values):
+            whole = torch.zeros(n + offset + 9, dtype=values.dtype, device=DEV)
+            whole[offset:offset + n] = values
+            return whole[offset:offset + n], whole
+
+        self.W, self.wholeW = buffer(draw(n, seed, wdt, 0.05))
+        self.G, _ = buffer(draw(n, seed + 1, gdt, 0.01))
+        m, v = draw(n, seed + 2, F32, 0.001), draw(n, seed + 3, F32, 0.01).square_() * torch.exp(draw(n, seed + 4, F32, 2.0))
+        if zero:
+            m, v = torch.zeros_like(m), torch.zeros_like(v)
+        self.m, self.v = m.cpu().numpy(), v.cpu().numpy()
+        self.mscale = self.vscale = None
+        if q8:
+            (cm, sm), (cv, sv) = adamw_ref.encode(self.m, 1, "M"), adamw_ref.encode(self.v, 1, "V")
+            self.m, self.v = adamw_ref.decode(cm, sm, "M"), adamw_ref.decode(cv, sv, "V")
+            up = lambda a: torch.from_numpy(a).to(DEV)  # noqa: E731
+            self.M, self.wholeM = buffer(up(cm))
+            self.V, self.wholeV = buffer(up(cv))
+            self.mscale, self.vscale = up(sm), up(sv)
+        else:
+            self.M, self.wholeM = buffer(m)
+            self.V, self.wholeV = buffer(v)
+        self.w = to_f64(self.W)
+
+    def check(self, t, scale=1.0, lr=LR, b1=B1, b2=B2, eps=EPS):
+        g = to_f64(self.G).astype(np.float32)
+        m, v = adamw_ref.moments(g, scale, self.m, self.v, b1, b2)
+        want, size = adamw_ref.update(self.w, m, v, lr, b1, b2, eps, t, self.decay)
+        half = torch.finfo(self.W.dtype).eps / 2 if self.W.dtype != F32 else 2.0 ** -24
+        got = to_f64(self.W)
+        fine = np.isfinite(want)
+        assert np.array_equal(np.isfinite(got), fine)
+        assert (np.abs(got - want)[fine] <= (half * np.abs(want) + FP32 * size)[fine]).all()
+        if self.q8:
+            (cm, sm), (cv, sv) = adamw_ref.encode(m, t, "M"), adamw_ref.encode(v, t, "V")
+            for have, code in ((self.M, cm), (self.V, cv)):
+                assert np.array_equal(have.cpu().numpy(), code)
+            for have, s in ((self.mscale, sm), (self.vscale, sv)):
+                assert np.array_equal(have.cpu().numpy(), s)
+            self.m, self.v = adamw_ref.decode(cm, sm, "M"), adamw_ref.decode(cv, sv, "V")
+        else:
+            assert np.array_equal(self.M.cpu().numpy(), m, equal_nan=True)
+            assert np.array_equal(self.V.cpu().numpy(), v, equal_nan=True)
+            self.m, self.v = m, v
+        for whole, n in ((self.wholeW, self.n), (self.wholeM, self.n), (self.wholeV, self.n)):
+            assert int((whole[-9:].float() != 0).sum()) == 0  # what lies behind is not touched
+        self.w = to_f64(self.W)
+
+
+def plan_of(tensors):
+    q8 = any(x.q8 for x in tensors)
+    e4, e5 = torch.float8_e4m3fn, torch.float8_e5m2
+    return grass.adamw_plan([x.W for x in tensors], [x.G for x in tensors],
+                            [x.M.view(e4) if x.q8 else x.M for x in tensors],
+                            [x.V.view(e5) if x.q8 else x.V for x in tensors], [x.decay for x in tensors],
+                            [x.mscale for x in tensors] if q8 else None, [x.vscale for x in tensors] if q8 else None)
+
+
+@pytest.mark.parametrize("q8", [False, True])
+@pytest.mark.parametrize("wdt,gdt", [(F32, F32), (F32, BF16), (BF16, F32), (BF16, BF16)])
+@pytest.mark.parametrize("offset", [0, 3])
+def test_step(wdt, gdt, q8, offset):
+    tensors = [Tensor(n, 10 * i, wdt, gdt, q8, offset if i % 2 else 0, 0.1 * (i % 3)) for i, n in enumerate(SIZES)]
+    plan = plan_of(tensors)
+    for t in (3, 4):
+        grass.adamw_step(plan, LR, B1, B2, EPS, t)
+        for x in tensors:
+            x.check(t)
+
+
+def test_all_types_in_one_plan_from_the_first_step():
+    kinds = [(w, g, q) for w in (F32, BF16) for g in (F32, BF16) for q in (False, True)]
+    tensors = [Tensor(300 + 17 * i, 10 * i, *k, zero=True, decay=0.05) for i, k in enumerate(kinds * 3)]
+    plan = plan_of(tensors)
+    for t in (1, 2, 3):
+        for x in tensors:
+            x.G.copy_(draw(x.n, 7 * t, x.G.dtype, 0.01 * t))
+        grass.adamw_step(plan, LR, B1, B2, EPS, t)
+        for x in tensors:
+            x.check(t)
+
+
+@pytest.mark.parametrize("q8", [False, True])
+def test_many_tensors(q8):
+    rng = np.random.default_rng(5)
+    tensors = [Tensor(int(n), 10 * i, BF16, BF16, q8, int(n) % 5) for i, n in enumerate(np.exp(rng.uniform(0, 9.5, 400)))]
+    grass.adamw_step(plan_of(tensors), LR, B1, B2, EPS, 100)
+    for x in tensors:
+        x.check(100)
+
+
+@pytest.mark.parametrize("q8", [False, True])
+def test_matrices_inside_larger_ones(q8):
+    """Rows of W and G with leading dimensions of their own; the moments are dense."""
+    rows, cols, ldw, ldg = 7, 256, 300, 259
+    x = Tensor(rows * cols, 1, BF16, F32, q8)
+    W, G = torch.zeros((rows, ldw), dtype=BF16, device=DEV), torch.zeros((rows, ldg), device=DEV)
+    W[:, :cols], G[:, :cols] = x.W.view(rows, cols), x.G.view(rows, cols)
+    keep = W[:, cols:].clone()
+    M, V = (x.M.view(torch.float8_e4m3fn), x.V.view(torch.float8_e5m2)) if q8 else (x.M, x.V)
+    plan = grass.adamw_plan([W[:, :cols]], [G[:, :cols]], [M], [V], 0.0, [x.mscale], [x.vscale])
+    grass.adamw_step(plan, LR, B1, B2, EPS, 9)
+    x.W.copy_(W[:, :cols].reshape(-1))
+    x.check(9)
+    assert torch.equal(W[:, cols:], keep)
+
+
+@pytest.mark.parametrize("q8", [False, True])
+def test_gradient_factor(q8):
+    x = Tensor(3000, 1, BF16, BF16, q8)
+    plan = plan_of([x])
+    grass.adamw_step(plan, LR, B1, B2, EPS, 5, grad_scale=torch.tensor([0.37], device=DEV))
+    x.check(5, scale=0.37)
+    was = [t.clone() for t in (x.W, x.M, x.V)]
+    grass.adamw_step(plan, LR, B1, B2, EPS, 6, grad_scale=torch.tensor([float("nan")], device=DEV))
+    assert all(torch.equal(a, b) for a, b in zip((x.W, x.M, x.V), was))  # the step was skipped
+
+
+@pytest.mark.parametrize("q8", [False, True])
+def test_gradients_that_are_not_finite_reach_their_own_element_alone(q8):
+    x = Tensor(1000, 1, F32, F32, q8)
+    for k, bad in ((5, math.inf), (200, math.nan), (999, -math.inf), (130, 1e30), (131, 1e-42)):
+        x.G[k] = bad
+    grass.adamw_step(plan_of([x]), LR, B1, B2, EPS, 5)
+    x.check(5)
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e-18, 1e-9, 1e12])
+def test_8_bit_moments_of_small_and_large_gradients(scale):
+    x = Tensor(1500, 1, F32, F32, True, zero=True)
+    x.G.mul_(scale)
+    plan = plan_of([x])
+    for t in (1, 2):
+        grass.adamw_step(plan, LR, B1, B2, 0.0 if scale > 1 else EPS, t)
+        x.check(t, eps=0.0 if scale > 1 else EPS)
+
+
+def test_blocks_that_are_zero_and_other_scales():
+    """A fresh state is zero codes under any finite scale; a block without gradients stays zero."""
+    x = Tensor(512, 1, BF16, BF16, True, zero=True)
+    x.mscale.fill_(123.0), x.vscale.fill_(0.0)
+    x.G[128:256] = 0
+    grass.adamw_step(plan_of([x]), LR, B1, B2, EPS, 1)
+    x.check(1)
+    assert int(x.M[128:256].sum()) == 0 and int(x.V[128:256].sum()) == 0
+
+
+def test_step_scalars_from_the_device_and_graph_replay():
+    tensors = [Tensor(n, 10 * i, BF16, F32, bool(i % 2)) for i, n in enumerate((4096, 4096, 333, 334))]
+    plan = plan_of(tensors)
+    scalars, out = torch.zeros(4, device=DEV), torch.zeros(2, device=DEV)
+    ws = grass.workspace(grass.grad_norm_workspace(plan))
+    state = [t for x in tensors for t in (x.W, x.M, x.V, *((x.mscale, x.vscale) if x.q8 else ()))]
+
+    def body():
+        grass.grad_norm(plan, 0.05, out, ws)
+        grass.adamw_step(plan, 9.0, B1, B2, EPS, 1, grad_scale=out[1:], step_scalars=scalars)
+
+    start = [t.clone() for t in state]
+    graph = torch.cuda.CUDAGraph()
+    scalars.copy_(torch.tensor(grass.adamw_step_scalars(LR, B1, B2, 20)))
+    body()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        body()
+    for t in (20, 21, 22):
+        for a, b in zip(state, start):
+            a.copy_(b)
+        grass.grad_norm(plan, 0.05, out, ws)
+        grass.adamw_step(plan, LR, B1, B2, EPS, t, grad_scale=out[1:])
+        want = [a.clone() for a in state]
+        for a, b in zip(state, start):
+            a.copy_(b)
+        out.fill_(float("nan"))
+        scalars.copy_(torch.tensor(grass.adamw_step_scalars(LR, B1, B2, t)))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(state, want))
+
+
+def test_side_stream():
+    a, b = (Tensor(5000, 1, BF16, BF16, True) for _ in range(2))
+    plans = plan_of([a]), plan_of([b])
+    grass.adamw_step(plans[0], LR, B1, B2, EPS, 5)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        grass.adamw_step(plans[1], LR, B1, B2, EPS, 5)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(a.W, b.W) and torch.equal(a.M, b.M)
+
+
+def test_empty_plans_and_tensors():
+    e = torch.empty(0, device=DEV)
+    for lists in (([], [], [], []), ([e], [e], [e], [e])):
+        plan = grass.adamw_plan(*lists)
+        grass.adamw_step(plan, LR, B1, B2, EPS, 1)
+        out = torch.full((2,), 5.0, device=DEV)
+        grass.grad_norm(plan, 1.0, out, grass.workspace(grass.grad_norm_workspace(plan)))
+        assert out.tolist() == [0.0, 1.0]
+
+
+def gpu_grad_norm(Gs, max_norm):
+    plan = grass.adamw_plan(None, Gs, None, None)
+    out = torch.full((2,), float("nan"), device=DEV)
+    ws = grass.workspace(grass.grad_norm_workspace(plan))
+    ws.fill_(0xFF)
+    grass.grad_norm(plan, max_norm, out, ws)
+    return out.tolist()
+
+
+@pytest.mark.parametrize("sizes", [[1], [7], [2048], [2049, 3], SIZES, [3000000, 5], [130] * 700])
+@pytest.mark.parametrize("scale", [1e-25, 0.01, 1e25])
+def test_grad_norm(sizes, scale):
+    Gs = [draw(n + 1, i, (F32, BF16)[i % 2], scale)[1:] for i, n in enumerate(sizes)]
+    want = math.sqrt(sum(float((g.double() ** 2).sum()) for g in Gs))
+    norm, factor = gpu_grad_norm(Gs, 0.5)
+    assert abs(norm - want) <= 2.0 ** -23 * want  # fp64 sums, rounded once to fp32
+    assert abs(factor - min(1.0, 0.5 / want)) <= 2.0 ** -23 * min(1.0, 0.5 / want)
+    assert (norm, factor) == tuple(gpu_grad_norm(Gs, 0.5))
+    # of a plan with weights, too
+    tensors = [Tensor(100 + i, i, BF16, BF16, bool(i % 2)) for i in range(5)]
+    plan, out = plan_of(tensors), torch.zeros(2, device=DEV)
+    grass.grad_norm(plan, 1e9, out, grass.workspace(grass.grad_norm_workspace(plan)))
+    want = math.sqrt(sum(float((x.G.double() ** 2).sum()) for x in tensors))
+    assert abs(out[0].item() - want) <= 2.0 ** -23 * want and out[1].item() == 1.0
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_grad_norm_of_gradients_that_are_not_finite(bad):
+    g = draw(5000, 1, F32)
+    g[4321] = bad
+    norm, factor = gpu_grad_norm([draw(10, 2, BF16), g], 1.0)
+    assert not math.isfinite(norm) and math.isnan(factor)

@@ -1,0 +1,177 @@
+"""What the norms, AdamW and the gradients' norm refuse on the host, before anything is launched, and how
+a plan is laid out (CPU only)."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2406_17660_amd import grass
+
+FAKE, ODD = 0x1000, 0x1001  # never dereferenced
+OK, NULL, SHAPE, DTYPE, WS = grass.OK, grass.ERR_NULL, grass.ERR_SHAPE, grass.ERR_DTYPE, grass.ERR_WORKSPACE
+NAN = float("nan")
+
+
+def call(f, names, values, **kw):
+    assert set(kw) <= set(names)
+    return f(*[kw.get(n, v) for n, v in zip(names, values)])
+
+
+def forward(**kw):
+    return call(grass.lib().grass_norm_forward,
+                "kind X ldx R ldr dt T n gain bias gdt eps H ldh Y ldy mean rstd stream".split(),
+                (0, FAKE, 64, FAKE, 64, 1, 8, 64, FAKE, FAKE, 0, 1e-5, FAKE, 64, FAKE, 64, FAKE, FAKE, None), **kw)
+
+
+@pytest.mark.parametrize("want,kw", [
+    (NULL, dict(X=None)), (NULL, dict(Y=None)), (NULL, dict(H=None)), (SHAPE, dict(T=-1)), (SHAPE, dict(n=0)), (SHAPE, dict(n=-5)),
+    (SHAPE, dict(T=1 << 31)), (SHAPE, dict(n=1 << 31)), (SHAPE, dict(ldx=63)), (SHAPE, dict(ldr=63)), (SHAPE, dict(ldh=63)),
+    (SHAPE, dict(ldy=63)), (SHAPE, dict(eps=-1.0)), (SHAPE, dict(eps=NAN)), (DTYPE, dict(kind=2)), (DTYPE, dict(dt=2)),
+    (DTYPE, dict(gdt=7)), (OK, dict(T=0)), (OK, dict(T=0, X=None, Y=None, H=None))])
+def test_norm_forward_validation(want, kw):
+    assert forward(**kw) == want
+
+
+def backward(**kw):
+    return call(grass.lib().grass_norm_backward,
+                "kind dY lddy H ldh dR lddr dt T n gain gdt mean rstd dX lddx dgain dbias ws ws_bytes stream".split(),
+                (0, FAKE, 64, FAKE, 64, FAKE, 64, 1, 8, 64, FAKE, 0, FAKE, FAKE, FAKE, 64, FAKE, FAKE, FAKE, 1 << 30, None), **kw)
+
+
+@pytest.mark.parametrize("want,kw", [
+    (NULL, dict(dY=None)), (NULL, dict(H=None)), (NULL, dict(mean=None)), (NULL, dict(rstd=None)), (NULL, dict(dX=None)),
+    (SHAPE, dict(T=-1)), (SHAPE, dict(n=0)), (SHAPE, dict(lddy=63)), (SHAPE, dict(ldh=63)), (SHAPE, dict(lddr=63)),
+    (SHAPE, dict(lddx=63)), (DTYPE, dict(kind=-1)), (DTYPE, dict(dt=9)), (DTYPE, dict(gdt=2)),
+    (WS, dict(ws=None)), (WS, dict(ws_bytes=16))])
+def test_norm_backward_validation(want, kw):
+    assert backward(**kw) == want
+
+
+def test_norm_backward_workspace():
+    q = grass.norm_backward_workspace
+    assert q(0, 100, grass.BF16) == 0 and q(-1, 4, grass.BF16) == 0 and q(4, 0, grass.BF16) == 0 and q(4, 4, 9) == 0
+    assert q(1, 100, grass.F32) >= 800
+    for T, n in ((7, 33), (1000, 4096), (131072, 512)):
+        need = q(T, n, grass.BF16)
+        assert backward(T=T, n=n, lddy=n, ldh=n, lddr=n, lddx=n, ws_bytes=need - 1) == WS
+
+
+def tensor(**kw):
+    a = grass.AdamWTensor(FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, 4, 100, 100, 100, grass.BF16, grass.F32, grass.MOMENTS_F32, 0.0)
+    for k, v in kw.items():
+        setattr(a, k, v)
+    return a
+
+
+def lay_out(*tensors):
+    arr = (grass.AdamWTensor * max(1, len(tensors)))(*tensors)
+    layout = grass.AdamWLayout()
+    n = grass.lib().grass_adamw_plan_bytes(len(tensors), arr)
+    host = (C.c_uint64 * max(1, n // 8))()
+    return grass.lib().grass_adamw_plan(len(tensors), arr, C.addressof(host), n, C.byref(layout)), layout, host, n
+
+
+@pytest.mark.parametrize("want,kw", [
+    (NULL, dict(W=None)), (NULL, dict(G=None)), (NULL, dict(M=None)), (NULL, dict(V=None)),
+    (NULL, dict(mscale=None, moments=1, cols=128, ldw=128, ldg=128)), (NULL, dict(vscale=None, moments=1)),
+    (SHAPE, dict(rows=-1)), (SHAPE, dict(cols=-1)), (SHAPE, dict(cols=1 << 31)), (SHAPE, dict(ldw=99)), (SHAPE, dict(ldg=99)),
+    (SHAPE, dict(W=ODD)), (SHAPE, dict(G=ODD)), (SHAPE, dict(G=FAKE + 2)), (SHAPE, dict(M=FAKE + 2)), (SHAPE, dict(V=ODD)),
+    (SHAPE, dict(moments=1, mscale=ODD)), (SHAPE, dict(moments=1, vscale=FAKE + 2)), (SHAPE, dict(moments=1, ldw=101)),
+    (DTYPE, dict(wdt=2)), (DTYPE, dict(gdt=-1)), (DTYPE, dict(moments=2)),
+    (OK, dict(moments=1, M=ODD, V=ODD)), (OK, dict(moments=1, ldw=101, rows=1)), (OK, dict(moments=1, cols=128, ldw=130, ldg=128)),
+    (OK, dict(W=None, M=None, V=None)), (OK, dict(rows=0, W=None, G=None, M=None, V=None))])
+def test_adamw_plan_validation(want, kw):
+    assert lay_out(tensor(), tensor(**kw))[0] == want
+
+
+def test_adamw_plan_covers_every_element_once():
+    """The chunks of a plan: addresses, lengths, types and decay of each, over dense tensors and rows."""
+    big = tensor(rows=3, cols=5000, ldw=5000, ldg=5000, weight_decay=0.5)
+    rows = tensor(W=0x100000, G=0x200000, M=0x300000, V=0x400000, mscale=0x500000, vscale=0x600000, rows=5, cols=2176, ldw=2200,
+                  ldg=2300, wdt=grass.F32, gdt=grass.BF16, moments=1)
+    grads = tensor(W=None, M=None, V=None, rows=1, cols=7, ldg=9)
+    st, layout, host, n = lay_out(big, rows, grads, tensor(rows=0, ldw=200))
+    assert st == OK and n == 64 * sum(layout.chunks)
+    words = [host[8 * k:8 * k + 8] for k in range(n // 64)]
+    seen = {"big": set(), "rows": set(), "grads": 0}
+    for W, G, M, V, ms, vs, packed, tail in words:
+        elems, gdt = packed & 0xFFFFFFFF, packed >> 32
+        assert 0 < elems <= 2048
+        if W == 0:
+            seen["grads"] += elems
+            assert G == FAKE
+        elif W < 0x100000:
+            at = (W - FAKE) // 2
+            assert G == FAKE + 4 * at and M == FAKE + 4 * at and V == M and ms == 0 and gdt == grass.F32
+            assert tail & 0xFFFFFFFF == 0x3F000000
+            seen["big"] |= set(range(at, at + elems))
+        else:
+            r, c = divmod((W - 0x100000) // 4, 2200)
+            at = r * 2176 + c
+            assert G == 0x200000 + 2 * (r * 2300 + c) and M == 0x300000 + at and V == 0x400000 + at and gdt == grass.BF16
+            assert at % 128 == 0 and ms == 0x500000 + at // 128 * 4 and vs == 0x600000 + at // 128 * 4
+            seen["rows"] |= set(range(at, at + elems))
+    assert seen == {"big": set(range(15000)), "rows": set(range(5 * 2176)), "grads": 7}
+
+
+def test_adamw_plan_needs_room_and_a_layout():
+    arr = (grass.AdamWTensor * 1)(tensor())
+    layout, L = grass.AdamWLayout(), grass.lib()
+    n = L.grass_adamw_plan_bytes(1, arr)
+    host = (C.c_uint64 * (n // 8))()
+    assert L.grass_adamw_plan(1, arr, C.addressof(host), n - 1, C.byref(layout)) == WS
+    assert L.grass_adamw_plan(1, arr, None, n, C.byref(layout)) == NULL
+    assert L.grass_adamw_plan(1, arr, C.addressof(host), n, None) == NULL
+    assert L.grass_adamw_plan(-1, arr, C.addressof(host), n, C.byref(layout)) == SHAPE
+    assert L.grass_adamw_plan(1, None, C.addressof(host), n, C.byref(layout)) == NULL
+    assert L.grass_adamw_plan(0, None, None, 0, C.byref(layout)) == OK and sum(layout.chunks) == 0
+    assert L.grass_adamw_plan_bytes(1, None) == 0
+
+
+def layout_of(*chunks):
+    a = grass.AdamWLayout()
+    for i, n in chunks:
+        a.chunks[i] = n
+    return C.byref(a)
+
+
+def step(**kw):
+    return call(grass.lib().grass_adamw_step, "plan layout lr b1 b2 eps t scalars scale stream".split(),
+                (FAKE, layout_of((0, 3)), 1e-3, 0.9, 0.999, 1e-8, 1, None, None, None), **kw)
+
+
+@pytest.mark.parametrize("want,kw", [
+    (NULL, dict(plan=None)), (NULL, dict(layout=None)), (SHAPE, dict(plan=FAKE + 8)), (SHAPE, dict(t=0)), (SHAPE, dict(b1=1.0)),
+    (SHAPE, dict(b1=-0.1)), (SHAPE, dict(b2=NAN)), (SHAPE, dict(layout=layout_of((0, -1)))), (SHAPE, dict(layout=layout_of((9, 1)))),
+    (OK, dict(layout=layout_of())), (OK, dict(layout=layout_of(), plan=None))])
+def test_adamw_step_validation(want, kw):
+    assert step(**kw) == want
+
+
+def norm(**kw):
+    return call(grass.lib().grass_grad_norm, "plan layout max_norm out ws ws_bytes stream".split(),
+                (FAKE, layout_of((0, 3), (8, 4)), 1.0, FAKE, FAKE, 1 << 20, None), **kw)
+
+
+@pytest.mark.parametrize("want,kw", [
+    (NULL, dict(plan=None)), (NULL, dict(layout=None)), (NULL, dict(out=None)), (SHAPE, dict(max_norm=-1.0)), (SHAPE, dict(max_norm=NAN)),
+    (WS, dict(ws=None)), (WS, dict(ws_bytes=8)), (WS, dict(ws=FAKE + 4))])
+def test_grad_norm_validation(want, kw):
+    assert norm(**kw) == want
+
+
+def test_step_scalars():
+    out = (C.c_float * 4)()
+    f = grass.lib().grass_adamw_step_scalars
+    assert f(1e-3, 0.9, 0.999, (1 << 24) + 7, out) == OK and out[3] == 7.0
+    assert list(out)[:3] == grass.adam_step_scalars(1e-3, 0.9, 0.999, (1 << 24) + 7)
+    assert f(1e-3, 0.9, 0.999, 0, out) == SHAPE and f(1e-3, 1.0, 0.999, 1, out) == SHAPE and f(1e-3, 0.9, 0.999, 1, None) == NULL
+
+
+def test_binding_refuses_host_tensors_and_other_types():
+    x = torch.zeros(4, 4)
+    with pytest.raises(AssertionError):
+        grass.norm_forward(x, None, None, 1e-5, x)
+    with pytest.raises(AssertionError):
+        grass.adamw_plan([x], [x], [x], [x])
+    assert grass.moment_blocks(0) == 0 and grass.moment_blocks(1) == 1 and grass.moment_blocks(129) == 2
