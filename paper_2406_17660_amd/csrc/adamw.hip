@@ -7,7 +7,7 @@
 // consecutive elements.  The 16 lanes that hold a block of 128 lie in one row of a wavefront, whose
 // lanes exchange values without LDS.
 #include "adam.hpp"
-#include "elem8.hpp"
+#include "elem.hpp"
 
 namespace grass {
 namespace {
@@ -58,7 +58,7 @@ struct StepArgs {
 struct MomentsF32 {
     float m[8], v[8];
     __device__ __forceinline__ void load(const Chunk& c, int at, int left) {
-        Raw8<float> a, b;
+        Raw<float, 8> a, b;
         const float *pm = static_cast<const float*>(c.M) + at, *pv = static_cast<const float*>(c.V) + at;
         if (left >= 8) {
             a.load_once(pm);
@@ -74,7 +74,7 @@ struct MomentsF32 {
         }
     }
     __device__ __forceinline__ void store(const Chunk& c, int at, int left, uint32_t) const {
-        Raw8<float> a, b;
+        Raw<float, 8> a, b;
         a.set(m);
         b.set(v);
         float *pm = static_cast<float*>(c.M) + at, *pv = static_cast<float*>(c.V) + at;
@@ -87,9 +87,6 @@ struct MomentsF32 {
         }
     }
 };
-
-typedef uint32_t raw2_t __attribute__((ext_vector_type(2)));
-typedef raw2_t raw2_on1_t __attribute__((aligned(1)));
 
 // The largest of the 16 lanes of a row, in every one of them.
 template <int kRotate>
@@ -142,7 +139,7 @@ typedef Code8<2, 14, 15> CodeV;   // e5m2
 
 __device__ __forceinline__ raw2_t load_codes(const void* p, int at, int left) {
     const uint8_t* q = static_cast<const uint8_t*>(p) + at;
-    if (left >= 8) return __builtin_nontemporal_load(reinterpret_cast<const raw2_on1_t*>(q));
+    if (left >= 8) return __builtin_nontemporal_load(reinterpret_cast<const raw2_any_t*>(q));
     raw2_t r = {0, 0};
 #pragma unroll
     for (int i = 0; i < 8; ++i)
@@ -152,7 +149,7 @@ __device__ __forceinline__ raw2_t load_codes(const void* p, int at, int left) {
 __device__ __forceinline__ void store_codes(void* p, int at, int left, raw2_t r) {
     uint8_t* q = static_cast<uint8_t*>(p) + at;
     if (left >= 8) {
-        __builtin_nontemporal_store(r, reinterpret_cast<raw2_on1_t*>(q));
+        __builtin_nontemporal_store(r, reinterpret_cast<raw2_any_t*>(q));
         return;
     }
 #pragma unroll
@@ -196,8 +193,8 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(StepArgs a) {
     const float grad_scale = a.grad_scale ? *a.grad_scale : 1.0f;
     if (grad_scale != grad_scale) return;
     const int at = threadIdx.x * 8, left = c.elems - at;
-    Raw8<W> w;
-    Raw8<G> g;
+    Raw<W, 8> w;
+    Raw<G, 8> g;
     W* pw = static_cast<W*>(c.W) + at;
     const G* pg = static_cast<const G*>(c.G) + at;
     if (left >= 8) {
@@ -236,7 +233,7 @@ constexpr int kNormBlocks = 2048;
 template <typename G>
 __device__ __forceinline__ double squares(const Chunk& c) {
     const int at = threadIdx.x * 8, left = c.elems - at;
-    Raw8<G> g;
+    Raw<G, 8> g;
     if (left >= 8) g.load(static_cast<const G*>(c.G) + at);
     else g.load_some(static_cast<const G*>(c.G) + at, left);
     double s = 0.0;

@@ -497,7 +497,7 @@ grass_status grass_norm_forward(grass_norm kind, const void* X, int64_t ldx, con
 
 size_t grass_norm_backward_workspace(int64_t T, int64_t n, grass_dtype dt) {
     if (T < 0 || n < 1 || !small(T) || !small(n) || !dtype_ok(dt)) return 0;
-    return norm_backward_workspace_bytes(T, n);
+    return norm_backward_workspace_bytes(T, n, dt);
 }
 
 grass_status grass_norm_backward(grass_norm kind, const void* dY, int64_t lddy, const void* H,
@@ -511,7 +511,7 @@ grass_status grass_norm_backward(grass_norm kind, const void* dY, int64_t lddy, 
     if (!present(dY, T) || !present(H, T) || !present(rstd, T) || !present(dX, T) ||
         (kind == GRASS_NORM_LAYER && !present(mean, T)))
         return GRASS_ERR_NULL;
-    const size_t need = dgain || dbias ? norm_backward_workspace_bytes(T, n) : 0;
+    const size_t need = dgain || dbias ? norm_backward_workspace_bytes(T, n, dt) : 0;
     if (need > 0 && (!ws || ws_bytes < need)) return GRASS_ERR_WORKSPACE;
     return launch_norm_backward(kind, dY, lddy, H, ldh, dR, lddr, dt, T, n, gain, gdt, mean, rstd, dX, lddx, dgain,
                                 dbias, ws, as_stream(stream));

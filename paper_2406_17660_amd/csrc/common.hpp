@@ -294,7 +294,7 @@ grass_status launch_norm_forward(grass_norm kind, const void* X, int64_t ldx, co
                                  grass_dtype dt, int64_t T, int64_t n, const void* gain, const void* bias,
                                  grass_dtype gdt, float eps, void* H, int64_t ldh, void* Y, int64_t ldy,
                                  float* mean, float* rstd, hipStream_t s);
-size_t norm_backward_workspace_bytes(int64_t T, int64_t n);
+size_t norm_backward_workspace_bytes(int64_t T, int64_t n, grass_dtype dt);
 grass_status launch_norm_backward(grass_norm kind, const void* dY, int64_t lddy, const void* H, int64_t ldh,
                                   const void* dR, int64_t lddr, grass_dtype dt, int64_t T, int64_t n,
                                   const void* gain, grass_dtype gdt, const float* mean, const float* rstd,

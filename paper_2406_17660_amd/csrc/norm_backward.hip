@@ -1,0 +1,363 @@
+// grass_norm_backward: layer norm and RMS norm.
+//
+// Bound by memory: dY and H (and dR) are read once and dX is written once.  A row stays in the
+// registers of the threads that share it between the two sums it needs and its outputs; the sums of
+// dgain and dbias over the rows stay in the registers of the threads that own the columns, for all
+// rows that a workgroup takes, and a second kernel adds the workgroups' sums.
+#include <type_traits>
+
+#include "elem.hpp"
+
+namespace grass {
+namespace {
+
+struct BackwardArgs {
+    const void *dY, *H, *dR, *gain;
+    void* dX;
+    int64_t lddy, ldh, lddr, lddx, T;
+    int n;
+    bool centre, gain_bf16, want_bias;
+    const float *mean, *rstd;
+    float* part;  // [gridDim.x][2][n]: sums of dY * xh and of dY over a block's rows, or nullptr
+};
+
+template <int N>
+__device__ __forceinline__ void load_gain(const BackwardArgs& a, int at, float (&g)[N]) {
+    if (!a.gain) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) g[i] = 1.f;
+    } else if (a.gain_bf16) {
+        Raw<uint16_t, N> r;
+        r.load(static_cast<const uint16_t*>(a.gain) + at);
+#pragma unroll
+        for (int i = 0; i < N; ++i) g[i] = r.get(i);
+    } else {
+        Raw<float, N> r;
+        r.load(static_cast<const float*>(a.gain) + at);
+#pragma unroll
+        for (int i = 0; i < N; ++i) g[i] = r.get(i);
+    }
+}
+
+// What a thread holds of a row.  kWindow: rows of whole 16-byte vectors that start on 16 bytes, through
+// windows; else rows in any position.
+template <typename T, int TPR, int V, bool kWindow, bool kAdd, bool kOnce>
+struct Row {
+    static constexpr int N = 16 / sizeof(T);
+    Raw<T, N> y[V], x[V], b[kAdd ? V : 1];
+    float mean, rstd;
+    __device__ __forceinline__ void load(const BackwardArgs& a, int64_t t, int lane, const Span (&at)[V]) {
+        const uint32_t bytes = t < a.T ? static_cast<uint32_t>(a.n) * sizeof(T) : 0u;
+        t = t < a.T ? t : a.T - 1;
+        const T* dy = static_cast<const T*>(a.dY) + t * a.lddy;
+        const T* h = static_cast<const T*>(a.H) + t * a.ldh;
+        const T* dr = static_cast<const T*>(a.dR) + t * a.lddr;
+        mean = (a.centre ? a.mean : a.rstd)[t];
+        rstd = a.rstd[t];
+        if constexpr (kWindow) {
+            const RowWindow wy(dy, bytes), wx(h, bytes);
+#pragma unroll
+            for (int v = 0; v < V; ++v) wy.template load<kOnce>(y[v].w, (v * TPR + lane) * 16);
+#pragma unroll
+            for (int v = 0; v < V; ++v) wx.template load<kOnce>(x[v].w, (v * TPR + lane) * 16);
+            if constexpr (kAdd) {
+                const RowWindow wb(dr, bytes);
+#pragma unroll
+                for (int v = 0; v < V; ++v) wb.template load<kOnce>(b[v].w, (v * TPR + lane) * 16);
+            }
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                y[v].template load_as<kOnce>(dy + at[v].at);
+                x[v].template load_as<kOnce>(h + at[v].at);
+                if constexpr (kAdd) b[v].template load_as<kOnce>(dr + at[v].at);
+            }
+        }
+    }
+};
+
+// A block's B / TPR row groups take rows from blockIdx on, gridDim apart.  While a thread works on its part
+// of one row, its part of the next is on its way.
+template <typename T, typename Shape, bool kWindow, bool kAdd, bool kOnce>
+__global__ __launch_bounds__(Shape::B) void backward_kernel(BackwardArgs a) {
+    constexpr int TPR = Shape::TPR, V = Shape::V, B = Shape::B, N = 16 / sizeof(T), kRows = B / TPR;
+    typedef Row<T, TPR, V, kWindow, kAdd, kOnce> RowPart;
+    __shared__ float red[2][B / kWave][2];
+    __shared__ float sums[B * N];
+    RowSum<TPR, B, 2> row_sum{red};
+    const int l = threadIdx.x % TPR;
+    const int group = TPR >= kWave ? __builtin_amdgcn_readfirstlane(threadIdx.x / TPR) : threadIdx.x / TPR;
+    const float inv_n = 1.0f / static_cast<float>(a.n);
+    Span at[V];
+    float gain[V][N], dgain[V][N], dbias[V][N];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        at[v] = span<TPR, N>(v, l, a.n);
+        load_gain<N>(a, at[v].at, gain[v]);
+#pragma unroll
+        for (int i = 0; i < N; ++i) dgain[v][i] = dbias[v][i] = 0.f;
+    }
+    const int64_t step = static_cast<int64_t>(gridDim.x) * kRows;
+    int64_t t0 = static_cast<int64_t>(blockIdx.x) * kRows;
+    const auto work = [&](const RowPart& row, int64_t t) {
+        const bool there = kRows == 1 || t < a.T;
+        const float mean = a.centre ? row.mean : 0.f, rstd = row.rstd;
+        float s[2] = {0.f, 0.f};
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int skip = there ? at[v].skip : N;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const bool own = kWindow || i >= skip;  // (behind a window's end there are zeros)
+                const float d = own ? row.y[v].get(i) : 0.f;
+                const float xh = own ? (row.x[v].get(i) - mean) * rstd : 0.f, z = d * gain[v][i];
+                s[0] += z * xh;
+                s[1] += z;
+                dgain[v][i] += d * xh;
+                dbias[v][i] += d;
+            }
+        }
+        // (behind row_sum all threads of the row have what they read of it, so that dX may lie over it)
+        row_sum(s);
+        const float c0 = s[0] * inv_n, c1 = a.centre ? s[1] * inv_n : 0.f;
+        T* dx = static_cast<T*>(a.dX) + t * a.lddx;
+        const RowWindow window(dx, there ? static_cast<uint32_t>(a.n) * sizeof(T) : 0u);
+        if (!kWindow && !there) return;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            float o[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float xh = (row.x[v].get(i) - mean) * rstd;
+                o[i] = rstd * (row.y[v].get(i) * gain[v][i] - c1 - xh * c0);
+                if constexpr (kAdd) o[i] += row.b[v].get(i);
+            }
+            Raw<T, N> out;
+            out.set(o);
+            if constexpr (kWindow) window.template store<kOnce>(out.w, (v * TPR + l) * 16);
+            else out.template store_as<kOnce>(dx + at[v].at);
+        }
+    };
+    // (the same number of turns for every thread: they meet at the barriers of row_sum)
+    RowPart even, odd;
+    even.load(a, t0 + group, l, at);
+    for (;; t0 += 2 * step) {
+        odd.load(a, t0 + step + group, l, at);
+        work(even, t0 + group);
+        if (t0 + step >= a.T) break;
+        even.load(a, t0 + 2 * step + group, l, at);
+        work(odd, t0 + step + group);
+        if (t0 + 2 * step >= a.T) break;
+    }
+    if (!a.part) return;
+    float* part = a.part + static_cast<int64_t>(blockIdx.x) * 2 * a.n;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        if (q == 1 && !a.want_bias) break;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            __syncthreads();
+            // a column's sums stand where its own thread's element would without the shift at the row's end
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (kWindow || i >= at[v].skip)
+                    sums[(group * TPR + l) * N + i - (kWindow ? 0 : at[v].skip)] = q ? dbias[v][i] : dgain[v][i];
+            __syncthreads();
+            for (int c = threadIdx.x; c < TPR * N; c += B) {
+                float s = sums[c];
+#pragma unroll
+                for (int r = 1; r < kRows; ++r) s += sums[r * TPR * N + c];
+                if (v * TPR * N + c < a.n) part[static_cast<int64_t>(q) * a.n + v * TPR * N + c] = s;
+            }
+        }
+    }
+}
+
+constexpr int kWide = 256;  // threads of the kernels for rows of any width
+
+// Rows of any width.  First the columns' sums (a block: 2048 columns of every gridDim.y-th row) ...
+template <typename T>
+__global__ __launch_bounds__(kWide) void backward_wide_sums_kernel(BackwardArgs a) {
+    const int64_t c = (static_cast<int64_t>(blockIdx.x) * kWide + threadIdx.x) * 8;
+    if (c >= a.n) return;
+    const int left = static_cast<int>(a.n - c < 8 ? a.n - c : 8);
+    float dgain[8] = {}, dbias[8] = {};
+    for (int64_t t = blockIdx.y; t < a.T; t += gridDim.y) {
+        Raw<T, 8> y, x;
+        const T *dy = static_cast<const T*>(a.dY) + t * a.lddy + c, *h = static_cast<const T*>(a.H) + t * a.ldh + c;
+        if (left == 8) {
+            y.load(dy);
+            x.load(h);
+        } else {
+            y.load_some(dy, left);
+            x.load_some(h, left);
+        }
+        const float mean = a.centre ? a.mean[t] : 0.f, rstd = a.rstd[t];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            dgain[i] += y.get(i) * ((x.get(i) - mean) * rstd);
+            dbias[i] += y.get(i);
+        }
+    }
+    float* part = a.part + static_cast<int64_t>(blockIdx.y) * 2 * a.n + c;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < left) {
+            part[i] = dgain[i];
+            if (a.want_bias) part[a.n + i] = dbias[i];
+        }
+}
+
+// ... then dX, a row per block at a time and a pass over it for each of the sums and the outputs.
+template <typename T>
+__global__ __launch_bounds__(kWide) void backward_wide_kernel(BackwardArgs a) {
+    __shared__ float red[2][kWide / kWave][2];
+    RowSum<kWide, kWide, 2> row_sum{red};
+    for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x) {
+        const float mean = a.centre ? a.mean[t] : 0.f, rstd = a.rstd[t];
+        float s[2] = {0.f, 0.f};
+        float c0 = 0.f, c1 = 0.f;
+        for (int pass = 0; pass < 2; ++pass) {
+            for (int64_t c = threadIdx.x * 8; c < a.n; c += kWide * 8) {
+                const int left = static_cast<int>(a.n - c < 8 ? a.n - c : 8);
+                const T *dy = static_cast<const T*>(a.dY) + t * a.lddy + c, *h = static_cast<const T*>(a.H) + t * a.ldh + c;
+                const T* dr = static_cast<const T*>(a.dR) + t * a.lddr + c;
+                const bool add = pass && a.dR;
+                Raw<T, 8> y, x, b;
+                b.zero();
+                float g[8];
+                if (left == 8) {
+                    y.load(dy);
+                    x.load(h);
+                    if (add) b.load(dr);
+                    load_gain<8>(a, static_cast<int>(c), g);
+                } else {
+                    y.load_some(dy, left);
+                    x.load_some(h, left);
+                    if (add) b.load_some(dr, left);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        g[i] = 1.f;
+                        if (a.gain && i < left)
+                            g[i] = a.gain_bf16 ? bf16_to_f32(static_cast<const uint16_t*>(a.gain)[c + i])
+                                               : static_cast<const float*>(a.gain)[c + i];
+                    }
+                }
+                float o[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float xh = (x.get(i) - mean) * rstd, z = y.get(i) * g[i];
+                    if (!pass && i < left) {
+                        s[0] += z * xh;
+                        s[1] += z;
+                    }
+                    o[i] = rstd * (z - c1 - xh * c0) + b.get(i);
+                }
+                if (!pass) continue;
+                x.set(o);
+                T* dx = static_cast<T*>(a.dX) + t * a.lddx + c;
+                if (left == 8) x.store(dx);
+                else x.store_some(dx, left);
+            }
+            if (pass) break;
+            row_sum(s);
+            c0 = s[0] / static_cast<float>(a.n);
+            c1 = a.centre ? s[1] / static_cast<float>(a.n) : 0.f;
+        }
+    }
+}
+
+// dgain and dbias from the P blocks' sums.  A block: 64 columns; its sixteen wavefronts take every
+// sixteenth row each.  P = 0 writes zeros.
+constexpr int kSumWaves = 16;
+__global__ __launch_bounds__(kSumWaves* kWave) void column_sums_kernel(const float* __restrict__ part, int P, int n,
+                                                                       float* dgain, float* dbias) {
+    __shared__ float sums[kSumWaves][kWave];
+    float* out = blockIdx.y ? dbias : dgain;
+    if (!out) return;
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int64_t c = static_cast<int64_t>(blockIdx.x) * kWave + lane;
+    float s = 0.f;
+    if (c < n) {
+        const float* p = part + static_cast<int64_t>(blockIdx.y) * n + c;
+#pragma unroll 16
+        for (int k = wave; k < P; k += kSumWaves) s += p[static_cast<int64_t>(k) * 2 * n];
+    }
+    sums[wave][lane] = s;
+    __syncthreads();
+    if (wave != 0 || c >= n) return;
+    s = sums[0][lane];
+#pragma unroll
+    for (int w = 1; w < kSumWaves; ++w) s += sums[w][lane];
+    out[c] = s;
+}
+
+template <typename T>
+int64_t row_groups(int64_t n) {
+    int64_t rows = 1;
+    if (in_registers<T>(n)) by_shape<T>(n, [&](auto shape) { rows = decltype(shape)::B / decltype(shape)::TPR; });
+    return rows;
+}
+
+// Blocks, each of which leaves one row of column sums: one per compute unit.
+int backward_blocks(int64_t T, int64_t n, grass_dtype dt) {
+    const int64_t rows = dt == GRASS_F32 ? row_groups<float>(n) : row_groups<uint16_t>(n);
+    const int64_t want = (T + rows - 1) / rows;
+    return static_cast<int>(want < kUnits ? want : kUnits);
+}
+
+template <typename T>
+void launch(const BackwardArgs& a, hipStream_t s) {
+    const unsigned grid = static_cast<unsigned>(backward_blocks(a.T, a.n, sizeof(T) == 4 ? GRASS_F32 : GRASS_BF16));
+    if (!in_registers<T>(a.n)) {
+        if (a.part) {
+            const dim3 g(static_cast<unsigned>((a.n + int64_t{kWide} * 8 - 1) / (kWide * 8)), grid);
+            backward_wide_sums_kernel<T><<<g, kWide, 0, s>>>(a);
+        }
+        backward_wide_kernel<T><<<static_cast<unsigned>(a.T < kMostBlocks ? a.T : kMostBlocks), kWide, 0, s>>>(a);
+        return;
+    }
+    const auto on16 = [](const void* p, int64_t ld) { return aligned_to(p, 16) && ld * sizeof(T) % 16 == 0; };
+    const bool window = a.n * sizeof(T) % 16 == 0 && on16(a.dY, a.lddy) && on16(a.H, a.ldh) && on16(a.dX, a.lddx) &&
+                        (!a.dR || on16(a.dR, a.lddr));
+    const bool once = static_cast<double>(a.T) * a.n * sizeof(T) * (a.dR ? 4 : 3) > kLastLevel;
+    by_shape<T>(a.n, [&](auto shape) {
+        typedef decltype(shape) S;
+        const auto go = [&](auto win, auto add, auto stream) {
+            backward_kernel<T, S, decltype(win)::value, decltype(add)::value, decltype(stream)::value><<<grid, S::B, 0, s>>>(a);
+        };
+        const auto with_add = [&](auto win, auto add) { once ? go(win, add, std::true_type{}) : go(win, add, std::false_type{}); };
+        const auto with_window = [&](auto win) { a.dR ? with_add(win, std::true_type{}) : with_add(win, std::false_type{}); };
+        if constexpr (S::TPR >= kWave)
+            if (window) return with_window(std::true_type{});
+        with_window(std::false_type{});
+    });
+}
+
+}  // namespace
+
+size_t norm_backward_workspace_bytes(int64_t T, int64_t n, grass_dtype dt) {
+    return static_cast<size_t>(backward_blocks(T, n, dt)) * 2 * n * sizeof(float);
+}
+
+grass_status launch_norm_backward(grass_norm kind, const void* dY, int64_t lddy, const void* H, int64_t ldh,
+                                  const void* dR, int64_t lddr, grass_dtype dt, int64_t T, int64_t n,
+                                  const void* gain, grass_dtype gdt, const float* mean, const float* rstd,
+                                  void* dX, int64_t lddx, float* dgain, float* dbias, void* ws, hipStream_t s) {
+    const bool sums = dgain || dbias;
+    if (T == 0 && !sums) return GRASS_OK;
+    if (T > 0) {
+        const BackwardArgs a{dY, H, dR, gain, dX, lddy, ldh, lddr, lddx, T, static_cast<int>(n),
+                             kind == GRASS_NORM_LAYER, gdt == GRASS_BF16, dbias != nullptr, mean, rstd,
+                             sums ? static_cast<float*>(ws) : nullptr};
+        dt == GRASS_F32 ? launch<float>(a, s) : launch<uint16_t>(a, s);
+    }
+    if (sums) {
+        const dim3 grid(static_cast<unsigned>((n + kWave - 1) / kWave), 2);
+        column_sums_kernel<<<grid, kSumWaves * kWave, 0, s>>>(static_cast<const float*>(ws), backward_blocks(T, n, dt),
+                                                              static_cast<int>(n), dgain, dbias);
+    }
+    return launch_status();
+}
+
+}  // namespace grass

@@ -1,0 +1,292 @@
+// grass_norm_forward: layer norm and RMS norm.
+//
+// Bound by memory: X (and R) are read once and Y (and H) are written once.  A row stays in the registers of
+// the threads that share it from its sums to its outputs; gain and bias stay there for all rows that a
+// workgroup takes.
+#include <type_traits>
+
+#include "elem.hpp"
+
+namespace grass {
+namespace {
+
+struct ForwardArgs {
+    const void *X, *R, *gain, *bias;
+    void *H, *Y;
+    int64_t ldx, ldr, ldh, ldy, T;
+    int n;
+    bool centre, gain_bf16;
+    float eps;
+    float *mean, *rstd;
+};
+
+// N values of gain or bias from column `at` on; `without` where there is none.
+template <int N>
+__device__ __forceinline__ void load_vector(const void* p, bool bf16, int at, float without, float (&g)[N]) {
+    if (!p) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) g[i] = without;
+    } else if (bf16) {
+        Raw<uint16_t, N> r;
+        r.load(static_cast<const uint16_t*>(p) + at);
+#pragma unroll
+        for (int i = 0; i < N; ++i) g[i] = r.get(i);
+    } else {
+        Raw<float, N> r;
+        r.load(static_cast<const float*>(p) + at);
+#pragma unroll
+        for (int i = 0; i < N; ++i) g[i] = r.get(i);
+    }
+}
+
+// What a thread holds of a row.  kWindow: rows of whole 16-byte vectors that start on 16 bytes, through
+// windows; else rows in any position.
+template <typename T, int TPR, int V, bool kWindow, bool kAdd, bool kOnce>
+struct Row {
+    static constexpr int N = 16 / sizeof(T);
+    Raw<T, N> x[V], b[kAdd ? V : 1];
+    __device__ __forceinline__ void load(const ForwardArgs& a, int64_t t, int lane, const Span (&at)[V]) {
+        const uint32_t bytes = t < a.T ? static_cast<uint32_t>(a.n) * sizeof(T) : 0u;
+        t = t < a.T ? t : a.T - 1;
+        const T* x0 = static_cast<const T*>(a.X) + t * a.ldx;
+        const T* r0 = static_cast<const T*>(a.R) + t * a.ldr;
+        if constexpr (kWindow) {
+            const RowWindow wx(x0, bytes);
+#pragma unroll
+            for (int v = 0; v < V; ++v) wx.template load<kOnce>(x[v].w, (v * TPR + lane) * 16);
+            if constexpr (kAdd) {
+                const RowWindow wb(r0, bytes);
+#pragma unroll
+                for (int v = 0; v < V; ++v) wb.template load<kOnce>(b[v].w, (v * TPR + lane) * 16);
+            }
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                x[v].template load_as<kOnce>(x0 + at[v].at);
+                if constexpr (kAdd) b[v].template load_as<kOnce>(r0 + at[v].at);
+            }
+        }
+    }
+};
+
+// A block's B / TPR row groups take rows from blockIdx on, gridDim apart.  While a thread works on its part
+// of one row, its part of the next is on its way.
+template <typename T, typename Shape, bool kWindow, bool kAdd, bool kOnce>
+__global__ __launch_bounds__(Shape::B) void forward_kernel(ForwardArgs a) {
+    constexpr int TPR = Shape::TPR, V = Shape::V, B = Shape::B, N = 16 / sizeof(T), kRows = B / TPR;
+    typedef Row<T, TPR, V, kWindow, kAdd, kOnce> RowPart;
+    __shared__ float red[2][B / kWave][1];
+    RowSum<TPR, B, 1> row_sum{red};
+    const int l = threadIdx.x % TPR;
+    const int group = TPR >= kWave ? __builtin_amdgcn_readfirstlane(threadIdx.x / TPR) : threadIdx.x / TPR;
+    const float n = static_cast<float>(a.n);
+    const int64_t step = static_cast<int64_t>(gridDim.x) * kRows;
+    int64_t t0 = static_cast<int64_t>(blockIdx.x) * kRows;
+    Span at[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) at[v] = span<TPR, N>(v, l, a.n);
+    RowPart even, odd;
+    even.load(a, t0 + group, l, at);
+    float gain[V][N], bias[V][N];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        load_vector<N>(a.gain, a.gain_bf16, at[v].at, 1.f, gain[v]);
+        load_vector<N>(a.bias, a.gain_bf16, at[v].at, 0.f, bias[v]);
+    }
+    const auto work = [&](RowPart& row, int64_t t) {
+        const bool there = kRows == 1 || t < a.T;
+        if constexpr (kAdd) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                float s[N];
+#pragma unroll
+                for (int i = 0; i < N; ++i) s[i] = row.x[v].get(i) + row.b[v].get(i);
+                row.x[v].set(s);
+            }
+        }
+        float mean = 0.f;
+        if (a.centre) {
+            float s[1] = {0.f};
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int i = 0; i < N; ++i) s[0] += kWindow || i >= at[v].skip ? row.x[v].get(i) : 0.f;
+            row_sum(s);
+            mean = s[0] / n;
+        }
+        float q[1] = {0.f};
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float d = i >= at[v].skip ? row.x[v].get(i) - mean : 0.f;
+                q[0] += d * d;
+            }
+        // (behind row_sum all threads of the row have what they read of it, so that H and Y may lie over it)
+        row_sum(q);
+        const float rstd = 1.0f / sqrtf(q[0] / n + a.eps);
+        if (there && l == 0) {
+            if (a.centre && a.mean) a.mean[t] = mean;
+            if (a.rstd) a.rstd[t] = rstd;
+        }
+        T* h = static_cast<T*>(a.H) + t * a.ldh;
+        T* y = static_cast<T*>(a.Y) + t * a.ldy;
+        const uint32_t bytes = there ? static_cast<uint32_t>(a.n) * sizeof(T) : 0u;
+        const RowWindow wh(h, bytes), wy(y, bytes);
+        if (!kWindow && !there) return;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            if constexpr (kAdd) {
+                if constexpr (kWindow) wh.template store<kOnce>(row.x[v].w, (v * TPR + l) * 16);
+                else row.x[v].template store_as<kOnce>(h + at[v].at);
+            }
+            float o[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) o[i] = (row.x[v].get(i) - mean) * rstd * gain[v][i] + bias[v][i];
+            Raw<T, N> out;
+            out.set(o);
+            if constexpr (kWindow) wy.template store<kOnce>(out.w, (v * TPR + l) * 16);
+            else out.template store_as<kOnce>(y + at[v].at);
+        }
+    };
+    // (the same number of turns for every thread: they meet at the barriers of row_sum)
+    for (;; t0 += 2 * step) {
+        odd.load(a, t0 + step + group, l, at);
+        work(even, t0 + group);
+        if (t0 + step >= a.T) break;
+        even.load(a, t0 + 2 * step + group, l, at);
+        work(odd, t0 + step + group);
+        if (t0 + 2 * step >= a.T) break;
+    }
+}
+
+constexpr int kWide = 256;  // threads of the kernel for rows of any width
+
+// Rows of any width, one per block at a time: the sum, the squares about the mean and the outputs are a pass
+// each over the row (over H, where there is a residual branch: every thread reads what it wrote).
+template <typename T>
+__global__ __launch_bounds__(kWide) void forward_wide_kernel(ForwardArgs a) {
+    __shared__ float red[2][kWide / kWave][1];
+    RowSum<kWide, kWide, 1> row_sum{red};
+    const int n = a.n;
+    const auto load = [&](Raw<T, 8>& u, const T* p, int left) {
+        if (left == 8) u.load(p);
+        else u.load_some(p, left);
+    };
+    const auto store = [&](const Raw<T, 8>& u, T* p, int left) {
+        if (left == 8) u.store(p);
+        else u.store_some(p, left);
+    };
+    for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x) {
+        const T* x = static_cast<const T*>(a.X) + t * a.ldx;
+        const T* h = a.R ? static_cast<const T*>(a.H) + t * a.ldh : x;
+        float s[1] = {0.f};
+        if (a.centre || a.R)
+            for (int64_t c = threadIdx.x * 8; c < n; c += kWide * 8) {
+                const int left = static_cast<int>(n - c < 8 ? n - c : 8);
+                Raw<T, 8> u;
+                load(u, x + c, left);
+                if (a.R) {
+                    Raw<T, 8> b;
+                    load(b, static_cast<const T*>(a.R) + t * a.ldr + c, left);
+                    float z[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) z[i] = u.get(i) + b.get(i);
+                    u.set(z);
+                    store(u, static_cast<T*>(a.H) + t * a.ldh + c, left);
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s[0] += u.get(i);
+            }
+        float mean = 0.f;
+        if (a.centre) {
+            row_sum(s);
+            mean = s[0] / static_cast<float>(n);
+        }
+        float q[1] = {0.f};
+        for (int64_t c = threadIdx.x * 8; c < n; c += kWide * 8) {
+            const int left = static_cast<int>(n - c < 8 ? n - c : 8);
+            Raw<T, 8> u;
+            load(u, h + c, left);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < left) {
+                    const float d = u.get(i) - mean;
+                    q[0] += d * d;
+                }
+        }
+        row_sum(q);
+        const float rstd = 1.0f / sqrtf(q[0] / static_cast<float>(n) + a.eps);
+        if (threadIdx.x == 0) {
+            if (a.centre && a.mean) a.mean[t] = mean;
+            if (a.rstd) a.rstd[t] = rstd;
+        }
+        for (int64_t c = threadIdx.x * 8; c < n; c += kWide * 8) {
+            const int left = static_cast<int>(n - c < 8 ? n - c : 8);
+            Raw<T, 8> u;
+            load(u, h + c, left);
+            float g[8], b[8], o[8];
+            if (left == 8) {
+                load_vector<8>(a.gain, a.gain_bf16, static_cast<int>(c), 1.f, g);
+                load_vector<8>(a.bias, a.gain_bf16, static_cast<int>(c), 0.f, b);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const auto value = [&](const void* p, float without) {
+                        if (!p || i >= left) return without;
+                        return a.gain_bf16 ? bf16_to_f32(static_cast<const uint16_t*>(p)[c + i]) : static_cast<const float*>(p)[c + i];
+                    };
+                    g[i] = value(a.gain, 1.f);
+                    b[i] = value(a.bias, 0.f);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) o[i] = (u.get(i) - mean) * rstd * g[i] + b[i];
+            u.set(o);
+            store(u, static_cast<T*>(a.Y) + t * a.ldy + c, left);
+        }
+    }
+}
+
+constexpr int kForwardBlocks = 2 * kUnits;
+
+template <typename T>
+void launch(const ForwardArgs& a, hipStream_t s) {
+    if (!in_registers<T>(a.n)) {
+        forward_wide_kernel<T><<<static_cast<unsigned>(a.T < kMostBlocks ? a.T : kMostBlocks), kWide, 0, s>>>(a);
+        return;
+    }
+    const auto on16 = [](const void* p, int64_t ld) { return aligned_to(p, 16) && ld * sizeof(T) % 16 == 0; };
+    const bool window = a.n * sizeof(T) % 16 == 0 && on16(a.X, a.ldx) && on16(a.Y, a.ldy) &&
+                        (!a.R || (on16(a.R, a.ldr) && on16(a.H, a.ldh)));
+    const bool once = static_cast<double>(a.T) * a.n * sizeof(T) * (a.R ? 4 : 2) > kLastLevel;
+    by_shape<T>(a.n, [&](auto shape) {
+        typedef decltype(shape) S;
+        constexpr int64_t kRows = S::B / S::TPR;
+        const int64_t groups = (a.T + kRows - 1) / kRows, most = kForwardBlocks;
+        const unsigned grid = static_cast<unsigned>(groups < most ? groups : most);
+        const auto go = [&](auto win, auto add, auto stream) {
+            forward_kernel<T, S, decltype(win)::value, decltype(add)::value, decltype(stream)::value><<<grid, S::B, 0, s>>>(a);
+        };
+        const auto with_add = [&](auto win, auto add) { once ? go(win, add, std::true_type{}) : go(win, add, std::false_type{}); };
+        const auto with_window = [&](auto win) { a.R ? with_add(win, std::true_type{}) : with_add(win, std::false_type{}); };
+        if constexpr (S::TPR >= kWave)
+            if (window) return with_window(std::true_type{});
+        with_window(std::false_type{});
+    });
+}
+
+}  // namespace
+
+grass_status launch_norm_forward(grass_norm kind, const void* X, int64_t ldx, const void* R, int64_t ldr,
+                                 grass_dtype dt, int64_t T, int64_t n, const void* gain, const void* bias,
+                                 grass_dtype gdt, float eps, void* H, int64_t ldh, void* Y, int64_t ldy,
+                                 float* mean, float* rstd, hipStream_t s) {
+    if (T == 0) return GRASS_OK;
+    const ForwardArgs a{X, R, gain, bias, H, Y, ldx, ldr, ldh, ldy, T, static_cast<int>(n),
+                        kind == GRASS_NORM_LAYER, gdt == GRASS_BF16, eps, mean, rstd};
+    dt == GRASS_F32 ? launch<float>(a, s) : launch<uint16_t>(a, s);
+    return launch_status();
+}
+
+}  // namespace grass
