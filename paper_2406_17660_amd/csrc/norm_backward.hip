@@ -139,15 +139,23 @@ __global__ __launch_bounds__(Shape::B) void backward_kernel(BackwardArgs a) {
         }
     };
     // (the same number of turns for every thread: they meet at the barriers of row_sum)
-    RowPart even, odd;
-    even.load(a, t0 + group, l, at);
-    for (;; t0 += 2 * step) {
-        odd.load(a, t0 + step + group, l, at);
-        work(even, t0 + group);
-        if (t0 + step >= a.T) break;
-        even.load(a, t0 + 2 * step + group, l, at);
-        work(odd, t0 + step + group);
-        if (t0 + 2 * step >= a.T) break;
+    if constexpr (V <= 2) {
+        RowPart even, odd;
+        even.load(a, t0 + group, l, at);
+        for (;; t0 += 2 * step) {
+            odd.load(a, t0 + step + group, l, at);
+            work(even, t0 + group);
+            if (t0 + step >= a.T) break;
+            even.load(a, t0 + 2 * step + group, l, at);
+            work(odd, t0 + step + group);
+            if (t0 + 2 * step >= a.T) break;
+        }
+    } else {  // the widest rows: no registers for a second one, and enough of the first under way
+        for (; t0 < a.T; t0 += step) {
+            RowPart row;
+            row.load(a, t0 + group, l, at);
+            work(row, t0 + group);
+        }
     }
     if (!a.part) return;
     float* part = a.part + static_cast<int64_t>(blockIdx.x) * 2 * a.n;

@@ -8,6 +8,7 @@ stream.  A missing library is an error: there is no fallback path.
 """
 import ctypes as C
 import os
+import struct
 
 import torch  # imported before the library is loaded so that both share one HIP runtime
 
@@ -381,7 +382,7 @@ def _words(n):
     return _WORDS[n]
 
 
-assert C.sizeof(StepLayer) == 8 * len(StepLayer._fields_)
+assert C.sizeof(StepLayer) == 8 * len(StepLayer._fields_) and C.sizeof(AdamWTensor) == 96
 
 
 def step_group(dYs, X, idxs, rhos, Ms, Vs, Ws, lr, beta1, beta2, eps, t, alpha, ws, layout=DY_TxM,
@@ -576,39 +577,44 @@ def gather_rows(G, idx, rho, out):
     return out
 
 
-def _norm_vec(t, n, dtype=None):
-    """Address of a vector of n values, or None."""
+def _like(t, shape, dtype):
+    """(address, leading dimension) of a matrix of that shape and dtype with contiguous rows."""
+    assert t.is_cuda and t.dtype == dtype and t.shape == shape, "matrices of one shape and dtype on the GPU"
+    ld, step = t.stride()
+    T, n = shape
+    if T > 1 and n > 0:
+        assert step == 1 or n == 1, "rows must be contiguous"
+    elif ld < n:
+        ld = n
+    return t.data_ptr(), ld
+
+
+def _vector(t, n, dtype):
+    """Address of n contiguous values, or None."""
     if t is None:
         return None
-    assert t.is_cuda and t.shape == (n,) and t.is_contiguous() and (dtype is None or t.dtype == dtype)
+    assert t.is_cuda and t.dtype == dtype and t.shape == (n,) and t.is_contiguous()
     return t.data_ptr()
-
-
-def _norm_mat(t, T, n, dtype):
-    """(address, leading dimension) of a T x n matrix, or (None, n)."""
-    if t is None:
-        return None, n
-    p, rows, cols, ld = _mat(t)
-    assert (rows, cols) == (T, n) and t.dtype == dtype
-    return p, ld
-
-
-def _gain_dtype(gain, bias):
-    given = [t for t in (gain, bias) if t is not None]
-    assert len({t.dtype for t in given}) <= 1, "gain and bias have one dtype"
-    return _dtype(given[0]) if given else F32
 
 
 def norm_forward(X, gain, bias, eps, Y, kind=NORM_LAYER, R=None, H=None, mean=None, rstd=None):
     """Layer norm or RMS norm (kind) of the rows of X, or of X + R, which H then receives; mean and
     rstd: T floats for the backward pass, or None."""
-    pX, T, n, ldx = _mat(X)
-    pR, ldr = _norm_mat(R, T, n, X.dtype)
-    pH, ldh = _norm_mat(H, T, n, X.dtype)
-    pY, ldy = _norm_mat(Y, T, n, X.dtype)
-    _check(lib().grass_norm_forward(kind, pX, ldx, pR, ldr, _dtype(X), T, n, _norm_vec(gain, n), _norm_vec(bias, n),
-                                    _gain_dtype(gain, bias), eps, pH, ldh, pY, ldy, _norm_vec(mean, T, torch.float32),
-                                    _norm_vec(rstd, T, torch.float32), _stream()), "grass_norm_forward")
+    shape, dtype = X.shape, X.dtype
+    pX, ldx = _like(X, shape, dtype)
+    pY, ldy = _like(Y, shape, dtype)
+    T, n = shape
+    pR = pH = None
+    ldr = ldh = n
+    if R is not None:
+        pR, ldr = _like(R, shape, dtype)
+        pH, ldh = _like(H, shape, dtype)
+    one = gain if gain is not None else bias
+    gdtype = torch.float32 if one is None else one.dtype
+    _check(lib().grass_norm_forward(kind, pX, ldx, pR, ldr, _dtype(X), T, n, _vector(gain, n, gdtype),
+                                    _vector(bias, n, gdtype), F32 if one is None else _dtype(one), eps, pH, ldh, pY, ldy,
+                                    _vector(mean, T, torch.float32), _vector(rstd, T, torch.float32), _stream()),
+           "grass_norm_forward")
     return Y
 
 
@@ -619,16 +625,23 @@ def norm_backward_workspace(T, n, dtype) -> int:
 def norm_backward(dY, H, gain, mean, rstd, dX, dgain, dbias, ws, kind=NORM_LAYER, dR=None):
     """Backward pass of norm_forward: dX (plus dR where given), dgain and dbias (fp32, or None) from the
     rows H that were normed and the statistics that the forward pass kept."""
-    pY, T, n, lddy = _mat(dY)
-    pH, ldh = _norm_mat(H, T, n, dY.dtype)
-    pR, lddr = _norm_mat(dR, T, n, dY.dtype)
-    pX, lddx = _norm_mat(dX, T, n, dY.dtype)
+    shape, dtype, f32 = dY.shape, dY.dtype, torch.float32
+    pY, lddy = _like(dY, shape, dtype)
+    pH, ldh = _like(H, shape, dtype)
+    pX, lddx = _like(dX, shape, dtype)
+    T, n = shape
+    pR, lddr = (None, n) if dR is None else _like(dR, shape, dtype)
+    gdtype = f32 if gain is None else gain.dtype
     wp, wb = _ws(ws)
-    _check(lib().grass_norm_backward(kind, pY, lddy, pH, ldh, pR, lddr, _dtype(dY), T, n, _norm_vec(gain, n),
-                                     _gain_dtype(gain, None), _norm_vec(mean, T, torch.float32),
-                                     _norm_vec(rstd, T, torch.float32), pX, lddx, _norm_vec(dgain, n, torch.float32),
-                                     _norm_vec(dbias, n, torch.float32), wp, wb, _stream()), "grass_norm_backward")
+    _check(lib().grass_norm_backward(kind, pY, lddy, pH, ldh, pR, lddr, _dtype(dY), T, n, _vector(gain, n, gdtype),
+                                     F32 if gain is None else _dtype(gain), _vector(mean, T, f32), _vector(rstd, T, f32), pX, lddx,
+                                     _vector(dgain, n, f32), _vector(dbias, n, f32), wp, wb, _stream()),
+           "grass_norm_backward")
     return dX
+
+
+def _f32_bits(x):
+    return int.from_bytes(struct.pack("<f", x), "little")
 
 
 _MOMENTS = {torch.float32: (MOMENTS_F32, torch.float32), torch.float8_e4m3fn: (MOMENTS_Q8, torch.float8_e5m2)}
@@ -642,17 +655,17 @@ class AdamWPlan:
         self.plan, self.layout, self.tensors = plan, layout, tensors
 
 
-def _rows(t):
-    """(address, rows, cols, leading dimension) of a tensor as AdamW sees it: anything contiguous, or
-    a 2-D tensor with contiguous rows."""
-    assert t.is_cuda
-    if t.dim() == 2 and not t.is_contiguous():
-        return _mat(t)
-    assert t.is_contiguous(), "contiguous tensors, or matrices with contiguous rows"
-    n = t.numel()
-    if t.dim() == 2 and n > 0:
-        return t.data_ptr(), t.shape[0], t.shape[1], t.shape[1]
-    return t.data_ptr(), min(n, 1), n, n
+def _as_rows(W, G):
+    """(rows, cols, ldw, ldg) of a weight and its gradient: one row where both are contiguous (more where
+    a size would pass 2^31), else matrices with contiguous rows."""
+    n = G.numel()
+    if W.is_contiguous() and G.is_contiguous():
+        if n < 1 << 31 or G.dim() < 2:
+            return 1, n, n, n
+        cols = G.shape[-1]
+        return n // cols, cols, cols, cols
+    assert G.dim() == 2, "contiguous tensors, or matrices with contiguous rows"
+    return G.shape[0], G.shape[1], _mat(W)[3], _mat(G)[3]
 
 
 def adamw_plan(Ws, Gs, Ms, Vs, weight_decay=0.0, Mscales=None, Vscales=None):
@@ -660,29 +673,31 @@ def adamw_plan(Ws, Gs, Ms, Vs, weight_decay=0.0, Mscales=None, Vscales=None):
     the blocks' scales in Mscales and Vscales); weight_decay: one value or one per tensor.  Ws, Ms
     and Vs None: a plan of gradients for grad_norm alone."""
     count = len(Gs)
-    tensors = (AdamWTensor * max(count, 1))()
     decay = weight_decay if isinstance(weight_decay, (list, tuple)) else [weight_decay] * count
     alone = Ws is None
     assert len(decay) == count and (alone or len(Ws) == len(Ms) == len(Vs) == count)
-    for i, (a, G) in enumerate(zip(tensors, Gs)):
-        a.G, a.rows, a.cols, a.ldg = _rows(G)
-        a.gdt, a.weight_decay = _dtype(G), decay[i]
+    words = []  # of the grass_adamw_tensor array, 8 bytes each
+    for i, G in enumerate(Gs):
+        assert G.is_cuda
         if alone:
+            rows, cols, ldg, _ = _as_rows(G, G)
+            words += (0, G.data_ptr(), 0, 0, 0, 0, rows, cols, ldg, ldg, _dtype(G) << 32, 0)
             continue
         W, M, V = Ws[i], Ms[i], Vs[i]
-        assert W.shape == G.shape and M.numel() == V.numel() == G.numel(), "shapes differ"
-        a.W, rows, cols, a.ldw = _rows(W)
-        assert (rows, cols) == (a.rows, a.cols)
-        a.wdt = _dtype(W)
-        if M.dtype not in _MOMENTS or V.dtype != _MOMENTS[M.dtype][1]:
+        rows, cols, ldw, ldg = _as_rows(W, G)
+        n = rows * cols
+        assert W.is_cuda and W.shape == G.shape and M.numel() == V.numel() == n, "shapes differ"
+        kind, vdtype = _MOMENTS.get(M.dtype, (None, None))
+        if V.dtype != vdtype:
             raise TypeError(f"unsupported moments {M.dtype}, {V.dtype}")
-        for t in (M, V):
-            assert t.is_cuda and t.is_contiguous()
-        a.M, a.V, a.moments = M.data_ptr(), V.data_ptr(), _MOMENTS[M.dtype][0]
-        if a.moments == MOMENTS_Q8:
-            for t in (Mscales[i], Vscales[i]):
-                assert t.shape == (moment_blocks(W.numel()),)
-            a.mscale, a.vscale = _vec(Mscales[i], torch.float32), _vec(Vscales[i], torch.float32)
+        assert M.is_cuda and V.is_cuda and M.is_contiguous() and V.is_contiguous()
+        pms = pvs = 0
+        if kind == MOMENTS_Q8:
+            blocks = moment_blocks(n)
+            pms, pvs = _vector(Mscales[i], blocks, torch.float32), _vector(Vscales[i], blocks, torch.float32)
+        words += (W.data_ptr(), G.data_ptr(), M.data_ptr(), V.data_ptr(), pms, pvs, rows, cols, ldw, ldg,
+                  _dtype(W) | _dtype(G) << 32, kind | _f32_bits(decay[i]) << 32)
+    tensors = _words(max(len(words), 1))(*words)
     layout = AdamWLayout()
     host = torch.empty(int(lib().grass_adamw_plan_bytes(count, tensors)), dtype=torch.uint8)
     _check(lib().grass_adamw_plan(count, tensors, host.data_ptr(), host.nbytes, C.byref(layout)), "grass_adamw_plan")
