@@ -26,7 +26,7 @@ struct alignas(16) Chunk {
     int32_t elems;
     int32_t gdt;
     float weight_decay;
-    int32_t unused;
+    int32_t aligned;  // W, G, M and V start on 16 bytes
 };
 static_assert(sizeof(Chunk) == 64, "one load of sixteen dwords");
 
@@ -54,33 +54,37 @@ struct StepArgs {
     const float* grad_scale;
 };
 
-// Moments of eight elements: fp32 ...
+// Moments of N consecutive elements of a thread, V times over a chunk.  fp32: four, so that a wavefront's
+// access is one piece of memory ...
 struct MomentsF32 {
-    float m[8], v[8];
+    static constexpr int N = 4, V = 2;
+    float m[N], v[N];
+    template <bool kOnce>
     __device__ __forceinline__ void load(const Chunk& c, int at, int left) {
-        Raw<float, 8> a, b;
+        Raw<float, N> a, b;
         const float *pm = static_cast<const float*>(c.M) + at, *pv = static_cast<const float*>(c.V) + at;
-        if (left >= 8) {
-            a.load_once(pm);
-            b.load_once(pv);
+        if (left >= N) {
+            a.load_as<kOnce>(pm);
+            b.load_as<kOnce>(pv);
         } else {
             a.load_some(pm, left);
             b.load_some(pv, left);
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < N; ++i) {
             m[i] = a.get(i);
             v[i] = b.get(i);
         }
     }
+    template <bool kOnce>
     __device__ __forceinline__ void store(const Chunk& c, int at, int left, uint32_t) const {
-        Raw<float, 8> a, b;
+        Raw<float, N> a, b;
         a.set(m);
         b.set(v);
         float *pm = static_cast<float*>(c.M) + at, *pv = static_cast<float*>(c.V) + at;
-        if (left >= 8) {
-            a.store_once(pm);
-            b.store_once(pv);
+        if (left >= N) {
+            a.store_as<kOnce>(pm);
+            b.store_as<kOnce>(pv);
         } else {
             a.store_some(pm, left);
             b.store_some(pv, left);
@@ -137,19 +141,24 @@ struct Code8 {
 typedef Code8<3, 7, 7> CodeM;     // e4m3
 typedef Code8<2, 14, 15> CodeV;   // e5m2
 
+template <bool kOnce>
 __device__ __forceinline__ raw2_t load_codes(const void* p, int at, int left) {
     const uint8_t* q = static_cast<const uint8_t*>(p) + at;
-    if (left >= 8) return __builtin_nontemporal_load(reinterpret_cast<const raw2_any_t*>(q));
+    const raw2_any_t* whole = reinterpret_cast<const raw2_any_t*>(q);
+    if (left >= 8) return kOnce ? __builtin_nontemporal_load(whole) : *whole;
     raw2_t r = {0, 0};
 #pragma unroll
     for (int i = 0; i < 8; ++i)
         if (i < left) r[i / 4] |= static_cast<uint32_t>(q[i]) << (8 * (i & 3));
     return r;
 }
+template <bool kOnce>
 __device__ __forceinline__ void store_codes(void* p, int at, int left, raw2_t r) {
     uint8_t* q = static_cast<uint8_t*>(p) + at;
     if (left >= 8) {
-        __builtin_nontemporal_store(r, reinterpret_cast<raw2_any_t*>(q));
+        raw2_any_t* whole = reinterpret_cast<raw2_any_t*>(q);
+        if constexpr (kOnce) __builtin_nontemporal_store(r, whole);
+        else *whole = r;
         return;
     }
 #pragma unroll
@@ -159,9 +168,11 @@ __device__ __forceinline__ void store_codes(void* p, int at, int left, raw2_t r)
 
 // ... and 8 bits.  Every lane of the wavefront takes part in store(), those without elements too.
 struct MomentsQ8 {
-    float m[8], v[8];
+    static constexpr int N = 8, V = 1;
+    float m[N], v[N];
+    template <bool kOnce>
     __device__ __forceinline__ void load(const Chunk& c, int at, int left) {
-        const raw2_t a = load_codes(c.M, at, left), b = load_codes(c.V, at, left);
+        const raw2_t a = load_codes<kOnce>(c.M, at, left), b = load_codes<kOnce>(c.V, at, left);
         const float sm = left > 0 ? c.mscale[at / kQBlock] : 0.f, sv = left > 0 ? c.vscale[at / kQBlock] : 0.f;
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
@@ -171,13 +182,14 @@ struct MomentsQ8 {
             v[4 * w] = v0.x * sv; v[4 * w + 1] = v0.y * sv; v[4 * w + 2] = v1.x * sv; v[4 * w + 3] = v1.y * sv;
         }
     }
+    template <bool kOnce>
     __device__ __forceinline__ void store(const Chunk& c, int at, int left, uint32_t t) const {
         const uint32_t em = CodeM::exponent(m), ev = CodeV::exponent(v);
         const uint32_t j = static_cast<uint32_t>(at % kQBlock) * 0x9E3779B1u;
         const raw2_t a = CodeM::codes(m, em, j + t * 0x6A09E667u), b = CodeV::codes(v, ev, j + t * 0xBB67AE85u);
         if (left <= 0) return;
-        store_codes(c.M, at, left, a);
-        store_codes(c.V, at, left, b);
+        store_codes<kOnce>(c.M, at, left, a);
+        store_codes<kOnce>(c.V, at, left, b);
         if (at % kQBlock == 0) {
             c.mscale[at / kQBlock] = CodeM::scale(em);
             c.vscale[at / kQBlock] = CodeV::scale(ev);
@@ -185,6 +197,56 @@ struct MomentsQ8 {
     }
 };
 
+template <bool kOnce, typename W, typename G, typename Moments>
+__device__ __forceinline__ void step_chunk(const Chunk& c, const AdamParams& p, uint32_t t, float grad_scale) {
+    constexpr int N = Moments::N, V = Moments::V;
+    Raw<W, N> w[V];
+    Raw<G, N> g[V];
+    Moments s[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+        const int at = (k * kThreads + threadIdx.x) * N, left = c.elems - at;
+        const W* pw = static_cast<const W*>(c.W) + at;
+        const G* pg = static_cast<const G*>(c.G) + at;
+        if (left >= N) {
+            w[k].template load_as<kOnce>(pw);
+            g[k].template load_as<kOnce>(pg);
+        } else {
+            w[k].load_some(pw, left);
+            g[k].load_some(pg, left);
+        }
+        s[k].template load<kOnce>(c, at, left);
+    }
+    const float keep = 1.0f - p.lr * c.weight_decay;
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+        const int at = (k * kThreads + threadIdx.x) * N, left = c.elems - at;
+        float out[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            {
+#pragma clang fp contract(off)
+                const float x = g[k].get(i) * grad_scale;
+                const float m0 = p.b1 * s[k].m[i], m1 = p.one_minus_b1 * x;
+                const float v0 = p.b2 * s[k].v[i], v1 = p.one_minus_b2 * x;
+                s[k].m[i] = m0 + m1;
+                s[k].v[i] = v0 + v1 * x;
+            }
+            // hardware square root and reciprocal, as in adam_elem
+            const float step = p.lr * (s[k].m[i] * p.inv_c1) *
+                               __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(s[k].v[i] * p.inv_c2) + p.eps);
+            out[i] = w[k].get(i) * keep - step;
+        }
+        s[k].template store<kOnce>(c, at, left, t);
+        w[k].set(out);
+        W* pw = static_cast<W*>(c.W) + at;
+        if (left >= N) w[k].template store_as<kOnce>(pw);
+        else w[k].store_some(pw, left);
+    }
+}
+
+// One chunk per workgroup.  The streaming hint only where every access is one whole piece: lines that two
+// lanes share are then read twice.
 template <typename W, typename G, typename Moments>
 __global__ __launch_bounds__(kThreads) void adamw_kernel(StepArgs a) {
     const Chunk c = a.chunks[blockIdx.x];
@@ -192,55 +254,41 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(StepArgs a) {
     const uint32_t t = p.step_scalars ? static_cast<uint32_t>(p.step_scalars[3]) : a.t;
     const float grad_scale = a.grad_scale ? *a.grad_scale : 1.0f;
     if (grad_scale != grad_scale) return;
-    const int at = threadIdx.x * 8, left = c.elems - at;
-    Raw<W, 8> w;
-    Raw<G, 8> g;
-    W* pw = static_cast<W*>(c.W) + at;
-    const G* pg = static_cast<const G*>(c.G) + at;
-    if (left >= 8) {
-        w.load_once(pw);
-        g.load_once(pg);
-    } else {
-        w.load_some(pw, left);
-        g.load_some(pg, left);
-    }
-    Moments s;
-    s.load(c, at, left);
-    float out[8];
-    const float keep = 1.0f - p.lr * c.weight_decay;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        {
-#pragma clang fp contract(off)
-            const float x = g.get(i) * grad_scale;
-            const float m0 = p.b1 * s.m[i], m1 = p.one_minus_b1 * x;
-            const float v0 = p.b2 * s.v[i], v1 = p.one_minus_b2 * x;
-            s.m[i] = m0 + m1;
-            s.v[i] = v0 + v1 * x;
-        }
-        // hardware square root and reciprocal, as in adam_elem
-        const float step = p.lr * (s.m[i] * p.inv_c1) * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(s.v[i] * p.inv_c2) + p.eps);
-        out[i] = w.get(i) * keep - step;
-    }
-    s.store(c, at, left, t);
-    w.set(out);
-    if (left >= 8) w.store_once(pw);
-    else w.store_some(pw, left);
+    if (c.aligned) step_chunk<true, W, G, Moments>(c, p, t, grad_scale);
+    else step_chunk<false, W, G, Moments>(c, p, t, grad_scale);
 }
 
 constexpr int kNormBlocks = 2048;
 
-template <typename G>
-__device__ __forceinline__ double squares(const Chunk& c) {
-    const int at = threadIdx.x * 8, left = c.elems - at;
-    Raw<G, 8> g;
-    if (left >= 8) g.load(static_cast<const G*>(c.G) + at);
-    else g.load_some(static_cast<const G*>(c.G) + at, left);
-    double s = 0.0;
+// A thread's part of the gradients of a chunk, as it lies in memory.
+struct Gradients {
+    Raw<float, 8> x;  // (eight bf16 values in its first half)
+    __device__ __forceinline__ void load(const Chunk& c) {
+        const int at = threadIdx.x * 8, left = c.elems - at;
+        if (c.gdt == GRASS_F32) {
+            const float* p = static_cast<const float*>(c.G) + at;
+            if (left >= 8) x.load(p);
+            else x.load_some(p, left);
+        } else {
+            const uint16_t* p = static_cast<const uint16_t*>(c.G) + at;
+            Raw<uint16_t, 8> h;
+            if (left >= 8) h.load(p);
+            else h.load_some(p, left);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s += static_cast<double>(g.get(i)) * static_cast<double>(g.get(i));
-    return s;
-}
+            for (int i = 0; i < 4; ++i) x.w[i] = h.w[i];
+        }
+    }
+    __device__ __forceinline__ double squares(const Chunk& c) const {
+        double s = 0.0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float half = __uint_as_float((i & 1) ? x.w[i / 2] & 0xFFFF0000u : x.w[i / 2] << 16);
+            const double v = c.gdt == GRASS_F32 ? x.get(i) : half;
+            s += v * v;
+        }
+        return s;
+    }
+};
 
 __device__ __forceinline__ double block_sum(double s) {
     __shared__ double part[kThreads / kWave];
@@ -253,9 +301,15 @@ __device__ __forceinline__ double block_sum(double s) {
 
 __global__ __launch_bounds__(kThreads) void grad_squares_kernel(const Chunk* __restrict__ chunks, int64_t count, double* part) {
     double s = 0.0;
-    for (int64_t k = blockIdx.x; k < count; k += gridDim.x) {
-        const Chunk c = chunks[k];
-        s += c.gdt == GRASS_F32 ? squares<float>(c) : squares<uint16_t>(c);
+    // two chunks at a time, whose loads are under way together
+    for (int64_t k = blockIdx.x; k < count; k += 2 * static_cast<int64_t>(gridDim.x)) {
+        const bool two = k + gridDim.x < count;
+        const Chunk c0 = chunks[k], c1 = chunks[two ? k + gridDim.x : k];
+        Gradients g0, g1;
+        g0.load(c0);
+        g1.load(c1);
+        s += g0.squares(c0);
+        if (two) s += g1.squares(c1);
     }
     s = block_sum(s);
     if (threadIdx.x == 0) part[blockIdx.x] = s;
@@ -322,6 +376,7 @@ void adamw_lay_out(int count, const grass_adamw_tensor* tensors, const grass_ada
                     c.mscale = q8 ? a.mscale + s / kQBlock : nullptr;
                     c.vscale = q8 ? a.vscale + s / kQBlock : nullptr;
                     c.weight_decay = a.weight_decay;
+                    c.aligned = aligned_to(c.W, 16) && aligned_to(c.G, 16) && aligned_to(c.M, 16) && aligned_to(c.V, 16);
                 }
                 *out++ = c;
             }
