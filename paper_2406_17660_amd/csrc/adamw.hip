@@ -263,8 +263,8 @@ constexpr int kNormBlocks = 2048;
 // A thread's part of the gradients of a chunk, as it lies in memory.
 struct Gradients {
     Raw<float, 8> x;  // (eight bf16 values in its first half)
-    __device__ __forceinline__ void load(const Chunk& c) {
-        const int at = threadIdx.x * 8, left = c.elems - at;
+    __device__ __forceinline__ void load(const Chunk& c, int tid) {
+        const int at = tid * 8, left = c.elems - at;
         if (c.gdt == GRASS_F32) {
             const float* p = static_cast<const float*>(c.G) + at;
             if (left >= 8) x.load(p);
@@ -290,40 +290,63 @@ struct Gradients {
     }
 };
 
+// Sum over a block of B threads, in thread 0.
+template <int B>
 __device__ __forceinline__ double block_sum(double s) {
-    __shared__ double part[kThreads / kWave];
+    __shared__ double part[B / kWave];
 #pragma unroll
     for (int o = kWave / 2; o > 0; o >>= 1) s += __shfl_xor(s, o, kWave);
     if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = s;
     __syncthreads();
-    return (part[0] + part[1]) + (part[2] + part[3]);
+    s = part[0];
+#pragma unroll
+    for (int w = 1; w < B / kWave; ++w) s += part[w];
+    return s;
 }
 
-__global__ __launch_bounds__(kThreads) void grad_squares_kernel(const Chunk* __restrict__ chunks, int64_t count, double* part) {
+// Squares of the chunks first, first + step, ...: a thread's part of two at a time, whose loads are under
+// way together.
+__device__ __forceinline__ double squares_of(const Chunk* __restrict__ chunks, int64_t count, int64_t first, int64_t step) {
+    const int tid = threadIdx.x % kThreads;
     double s = 0.0;
-    // two chunks at a time, whose loads are under way together
-    for (int64_t k = blockIdx.x; k < count; k += 2 * static_cast<int64_t>(gridDim.x)) {
-        const bool two = k + gridDim.x < count;
-        const Chunk c0 = chunks[k], c1 = chunks[two ? k + gridDim.x : k];
+    for (int64_t k = first; k < count; k += 2 * step) {
+        const bool two = k + step < count;
+        const Chunk c0 = chunks[k], c1 = chunks[two ? k + step : k];
         Gradients g0, g1;
-        g0.load(c0);
-        g1.load(c1);
+        g0.load(c0, tid);
+        g1.load(c1, tid);
         s += g0.squares(c0);
         if (two) s += g1.squares(c1);
     }
-    s = block_sum(s);
+    return s;
+}
+
+__device__ __forceinline__ void write_norm(double s, float max_norm, float* out) {
+    const double norm = sqrt(s);
+    out[0] = static_cast<float>(norm);
+    const double factor = norm > static_cast<double>(max_norm) ? static_cast<double>(max_norm) / norm : 1.0;
+    out[1] = s <= 1.7976931348623157e308 ? static_cast<float>(factor) : __uint_as_float(0x7FC00000u);
+}
+
+__global__ __launch_bounds__(kThreads) void grad_squares_kernel(const Chunk* __restrict__ chunks, int64_t count, double* part) {
+    const double s = block_sum<kThreads>(squares_of(chunks, count, blockIdx.x, gridDim.x));
     if (threadIdx.x == 0) part[blockIdx.x] = s;
 }
 
 __global__ __launch_bounds__(kThreads) void grad_norm_kernel(const double* __restrict__ part, int count, float max_norm, float* out) {
     double s = 0.0;
     for (int k = threadIdx.x; k < count; k += kThreads) s += part[k];
-    s = block_sum(s);
-    if (threadIdx.x != 0) return;
-    const double norm = sqrt(s);
-    out[0] = static_cast<float>(norm);
-    const double factor = norm > static_cast<double>(max_norm) ? static_cast<double>(max_norm) / norm : 1.0;
-    out[1] = s <= 1.7976931348623157e308 ? static_cast<float>(factor) : __uint_as_float(0x7FC00000u);
+    s = block_sum<kThreads>(s);
+    if (threadIdx.x == 0) write_norm(s, max_norm, out);
+}
+
+// Few chunks: one block of four times the threads takes them all, in one launch.
+constexpr int kFewThreads = 4 * kThreads;
+constexpr int64_t kFewChunks = 16;
+__global__ __launch_bounds__(kFewThreads) void grad_norm_few_kernel(const Chunk* __restrict__ chunks, int count, float max_norm, float* out) {
+    const int group = __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads);
+    const double s = block_sum<kFewThreads>(squares_of(chunks, count, group, kFewThreads / kThreads));
+    if (threadIdx.x == 0) write_norm(s, max_norm, out);
 }
 
 int64_t chunks_in(const grass_adamw_layout& layout) {
@@ -429,9 +452,12 @@ grass_status launch_grad_norm(const void* plan, const grass_adamw_layout& layout
                               void* ws, hipStream_t s) {
     const int blocks = norm_blocks(layout);
     double* part = static_cast<double*>(ws);
-    if (blocks > 0)
-        grad_squares_kernel<<<static_cast<unsigned>(blocks), kThreads, 0, s>>>(static_cast<const Chunk*>(plan),
-                                                                               chunks_in(layout), part);
+    if (blocks <= kFewChunks) {
+        grad_norm_few_kernel<<<1, kFewThreads, 0, s>>>(static_cast<const Chunk*>(plan), blocks, max_norm, out);
+        return launch_status();
+    }
+    grad_squares_kernel<<<static_cast<unsigned>(blocks), kThreads, 0, s>>>(static_cast<const Chunk*>(plan),
+                                                                           chunks_in(layout), part);
     grad_norm_kernel<<<1, kThreads, 0, s>>>(part, blocks, max_norm, out);
     return launch_status();
 }

@@ -18,7 +18,9 @@ struct BackwardArgs {
     int n;
     bool centre, gain_bf16, want_bias;
     const float *mean, *rstd;
-    float* part;  // [gridDim.x][2][n]: sums of dY * xh and of dY over a block's rows, or nullptr
+    float* part;  // [blocks][2][n]: sums of dY * xh and of dY over a block's rows, or nullptr
+    unsigned column_blocks;  // the first blocks of the grid add up columns instead of taking rows
+    float *dgain, *dbias;    // what they write
 };
 
 template <int N>
@@ -76,14 +78,58 @@ struct Row {
     }
 };
 
-// A block's B / TPR row groups take rows from blockIdx on, gridDim apart.  While a thread works on its part
-// of one row, its part of the next is on its way.
+// Few rows: dgain and dbias of 64 vectors of columns, whole, by one block; its wavefronts take rows in turn.
+// (That reads dY and H twice, and spares the second kernel and what goes between the two.)
+template <typename T, int B>
+__device__ __forceinline__ void add_columns_up(const BackwardArgs& a, float* sums) {
+    constexpr int N = 16 / sizeof(T), kWaves = B / kWave;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * kWave * N;
+    const Span at = span<kWave, N>(0, lane, static_cast<int>(a.n - first < kWave * N ? a.n - first : kWave * N));
+    // (the row's last piece may be shorter than a vector, which then starts before it)
+    const T* dy = static_cast<const T*>(a.dY) + first + at.at;
+    const T* h = static_cast<const T*>(a.H) + first + at.at;
+    float dgain[N] = {}, dbias[N] = {};
+#pragma unroll 4
+    for (int64_t t = wave; t < a.T; t += kWaves) {
+        Raw<T, N> y, x;
+        y.load(dy + t * a.lddy);
+        x.load(h + t * a.ldh);
+        const float mean = a.centre ? a.mean[t] : 0.f, rstd = a.rstd[t];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            dgain[i] += y.get(i) * ((x.get(i) - mean) * rstd);
+            dbias[i] += y.get(i);
+        }
+    }
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        float* out = q ? a.dbias : a.dgain;
+        if (!out) continue;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i >= at.skip) sums[wave * kWave * N + lane * N + i - at.skip] = q ? dbias[i] : dgain[i];
+        __syncthreads();
+        for (int c = threadIdx.x; c < kWave * N; c += B) {
+            float s = sums[c];
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) s += sums[w * kWave * N + c];
+            if (first + c < a.n) out[first + c] = s;
+        }
+    }
+}
+
+// A block's B / TPR row groups take every so many-th row.  While a thread works on its part of one row, its
+// part of the next is on its way.
 template <typename T, typename Shape, bool kWindow, bool kAdd, bool kOnce>
 __global__ __launch_bounds__(Shape::B) void backward_kernel(BackwardArgs a) {
     constexpr int TPR = Shape::TPR, V = Shape::V, B = Shape::B, N = 16 / sizeof(T), kRows = B / TPR;
     typedef Row<T, TPR, V, kWindow, kAdd, kOnce> RowPart;
     __shared__ float red[2][B / kWave][2];
     __shared__ float sums[B * N];
+    if (blockIdx.x < a.column_blocks) return add_columns_up<T, B>(a, sums);
+    const unsigned block = blockIdx.x - a.column_blocks, blocks = gridDim.x - a.column_blocks;
     RowSum<TPR, B, 2> row_sum{red};
     const int l = threadIdx.x % TPR;
     const int group = TPR >= kWave ? __builtin_amdgcn_readfirstlane(threadIdx.x / TPR) : threadIdx.x / TPR;
@@ -97,8 +143,8 @@ __global__ __launch_bounds__(Shape::B) void backward_kernel(BackwardArgs a) {
 #pragma unroll
         for (int i = 0; i < N; ++i) dgain[v][i] = dbias[v][i] = 0.f;
     }
-    const int64_t step = static_cast<int64_t>(gridDim.x) * kRows;
-    int64_t t0 = static_cast<int64_t>(blockIdx.x) * kRows;
+    const int64_t step = static_cast<int64_t>(blocks) * kRows;
+    int64_t t0 = static_cast<int64_t>(block) * kRows;
     const auto work = [&](const RowPart& row, int64_t t) {
         const bool there = kRows == 1 || t < a.T;
         const float mean = a.centre ? row.mean : 0.f, rstd = row.rstd;
@@ -158,7 +204,7 @@ __global__ __launch_bounds__(Shape::B) void backward_kernel(BackwardArgs a) {
         }
     }
     if (!a.part) return;
-    float* part = a.part + static_cast<int64_t>(blockIdx.x) * 2 * a.n;
+    float* part = a.part + static_cast<int64_t>(block) * 2 * a.n;
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
         if (q == 1 && !a.want_bias) break;
@@ -314,32 +360,54 @@ int backward_blocks(int64_t T, int64_t n, grass_dtype dt) {
     return static_cast<int>(want < kUnits ? want : kUnits);
 }
 
+// Rows up to which dgain and dbias are added up beside dX in one launch.
+constexpr int64_t kFewRows = 64;
+
+// True where dgain and dbias are done with, false where the blocks' sums wait to be added.
 template <typename T>
-void launch(const BackwardArgs& a, hipStream_t s) {
-    const unsigned grid = static_cast<unsigned>(backward_blocks(a.T, a.n, sizeof(T) == 4 ? GRASS_F32 : GRASS_BF16));
+bool launch(BackwardArgs a, hipStream_t s) {
+    const unsigned rows = static_cast<unsigned>(backward_blocks(a.T, a.n, sizeof(T) == 4 ? GRASS_F32 : GRASS_BF16));
     if (!in_registers<T>(a.n)) {
         if (a.part) {
-            const dim3 g(static_cast<unsigned>((a.n + int64_t{kWide} * 8 - 1) / (kWide * 8)), grid);
+            const dim3 g(static_cast<unsigned>((a.n + int64_t{kWide} * 8 - 1) / (kWide * 8)), rows);
             backward_wide_sums_kernel<T><<<g, kWide, 0, s>>>(a);
         }
         backward_wide_kernel<T><<<static_cast<unsigned>(a.T < kMostBlocks ? a.T : kMostBlocks), kWide, 0, s>>>(a);
-        return;
+        return false;
     }
     const auto on16 = [](const void* p, int64_t ld) { return aligned_to(p, 16) && ld * sizeof(T) % 16 == 0; };
     const bool window = a.n * sizeof(T) % 16 == 0 && on16(a.dY, a.lddy) && on16(a.H, a.ldh) && on16(a.dX, a.lddx) &&
                         (!a.dR || on16(a.dR, a.lddr));
     const bool once = static_cast<double>(a.T) * a.n * sizeof(T) * (a.dR ? 4 : 3) > kLastLevel;
-    by_shape<T>(a.n, [&](auto shape) {
-        typedef decltype(shape) S;
-        const auto go = [&](auto win, auto add, auto stream) {
-            backward_kernel<T, S, decltype(win)::value, decltype(add)::value, decltype(stream)::value><<<grid, S::B, 0, s>>>(a);
-        };
-        const auto with_add = [&](auto win, auto add) { once ? go(win, add, std::true_type{}) : go(win, add, std::false_type{}); };
-        const auto with_window = [&](auto win) { a.dR ? with_add(win, std::true_type{}) : with_add(win, std::false_type{}); };
-        if constexpr (S::TPR >= kWave)
-            if (window) return with_window(std::true_type{});
-        with_window(std::false_type{});
-    });
+    const auto run = [&](unsigned column_blocks, unsigned row_blocks) {
+        a.column_blocks = column_blocks;
+        by_shape<T>(a.n, [&](auto shape) {
+            typedef decltype(shape) S;
+            const auto go = [&](auto win, auto add, auto stream) {
+                backward_kernel<T, S, decltype(win)::value, decltype(add)::value, decltype(stream)::value>
+                    <<<column_blocks + row_blocks, S::B, 0, s>>>(a);
+            };
+            const auto with_add = [&](auto win, auto add) { once ? go(win, add, std::true_type{}) : go(win, add, std::false_type{}); };
+            const auto with_window = [&](auto win) { a.dR ? with_add(win, std::true_type{}) : with_add(win, std::false_type{}); };
+            if constexpr (S::TPR >= kWave)
+                if (window) return with_window(std::true_type{});
+            with_window(std::false_type{});
+        });
+    };
+    if (!a.part || a.T > kFewRows) {
+        run(0, rows);
+        return false;
+    }
+    a.part = nullptr;
+    constexpr int kColumns = kWave * 16 / static_cast<int>(sizeof(T));
+    const unsigned columns = static_cast<unsigned>((a.n + kColumns - 1) / kColumns);
+    if (a.dX != a.dY && a.dX != a.H) {
+        run(columns, rows);
+    } else {  // dX overwrites what the columns' sums read
+        run(columns, 0);
+        run(0, rows);
+    }
+    return true;
 }
 
 }  // namespace
@@ -354,13 +422,14 @@ grass_status launch_norm_backward(grass_norm kind, const void* dY, int64_t lddy,
                                   void* dX, int64_t lddx, float* dgain, float* dbias, void* ws, hipStream_t s) {
     const bool sums = dgain || dbias;
     if (T == 0 && !sums) return GRASS_OK;
+    bool done = !sums;
     if (T > 0) {
         const BackwardArgs a{dY, H, dR, gain, dX, lddy, ldh, lddr, lddx, T, static_cast<int>(n),
                              kind == GRASS_NORM_LAYER, gdt == GRASS_BF16, dbias != nullptr, mean, rstd,
-                             sums ? static_cast<float*>(ws) : nullptr};
-        dt == GRASS_F32 ? launch<float>(a, s) : launch<uint16_t>(a, s);
+                             sums ? static_cast<float*>(ws) : nullptr, 0, dgain, dbias};
+        done = (dt == GRASS_F32 ? launch<float>(a, s) : launch<uint16_t>(a, s)) || done;
     }
-    if (sums) {
+    if (!done) {
         const dim3 grid(static_cast<unsigned>((n + kWave - 1) / kWave), 2);
         column_sums_kernel<<<grid, kSumWaves * kWave, 0, s>>>(static_cast<const float*>(ws), backward_blocks(T, n, dt),
                                                               static_cast<int>(n), dgain, dbias);
