@@ -342,7 +342,7 @@ __global__ __launch_bounds__(kThreads) void grad_norm_kernel(const double* __res
 
 // Few chunks: one block of four times the threads takes them all, in one launch.
 constexpr int kFewThreads = 4 * kThreads;
-constexpr int64_t kFewChunks = 16;
+constexpr int64_t kFewChunks = 32;
 __global__ __launch_bounds__(kFewThreads) void grad_norm_few_kernel(const Chunk* __restrict__ chunks, int count, float max_norm, float* out) {
     const int group = __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads);
     const double s = block_sum<kFewThreads>(squares_of(chunks, count, group, kFewThreads / kThreads));

@@ -189,14 +189,14 @@ struct RowSum {
 // share: every vector is read and written whole.  The one that would end behind the row is the row's
 // last N values instead, whose first `skip` are the thread before's too: both compute and write the
 // same there, and sums leave them out here.  A vector without values of its own (skip = N) is another
-// copy of the row's last.
+// copy of the row's last.  With V > 1 vectors per thread the row fills the first half of them (see by_shape).
 struct Span {
     int at, skip;
 };
-template <int TPR, int N>
+template <int TPR, int V, int N>
 __device__ __forceinline__ Span span(int v, int lane, int n) {
     const int c = (v * TPR + lane) * N;
-    if (c + N <= n) return {c, 0};
+    if (v < V / 2 || c + N <= n) return {c, 0};
     return {n - N, c < n ? c - (n - N) : N};
 }
 
@@ -205,7 +205,7 @@ template <int TPR_, int V_>
 struct RowShape {
     static constexpr int TPR = TPR_, V = V_, B = 512;
 };
-constexpr int kWidestRow = 32768;  // bytes of a row that stay in registers
+constexpr int kWidestRow = 16384;  // values of a row that stay in registers
 // The shape for a row of n values, as a call of f with it.  Two vectors per thread, so that a workgroup
 // has 16 KB of each array under way; more for the widest rows, one for the narrowest.
 template <typename T, typename F>
@@ -217,10 +217,11 @@ void by_shape(int64_t n, F&& f) {
     else if (vectors <= 256) f(RowShape<128, 2>{});
     else if (vectors <= 512) f(RowShape<256, 2>{});
     else if (vectors <= 1024) f(RowShape<512, 2>{});
-    else f(RowShape<512, 4>{});
+    else if (vectors <= 2048) f(RowShape<512, 4>{});
+    else if constexpr (sizeof(T) == 4) f(RowShape<512, 8>{});
 }
 template <typename T>
-bool in_registers(int64_t n) { return n * sizeof(T) >= 16 && n * sizeof(T) <= kWidestRow; }
+bool in_registers(int64_t n) { return n >= static_cast<int64_t>(16 / sizeof(T)) && n <= kWidestRow; }
 
 constexpr int kUnits = 256;                         // compute units
 constexpr double kLastLevel = 256.0 * (1 << 20);     // bytes of the last-level cache

@@ -85,7 +85,7 @@ __device__ __forceinline__ void add_columns_up(const BackwardArgs& a, float* sum
     constexpr int N = 16 / sizeof(T), kWaves = B / kWave;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     const int64_t first = static_cast<int64_t>(blockIdx.x) * kWave * N;
-    const Span at = span<kWave, N>(0, lane, static_cast<int>(a.n - first < kWave * N ? a.n - first : kWave * N));
+    const Span at = span<kWave, 1, N>(0, lane, static_cast<int>(a.n - first < kWave * N ? a.n - first : kWave * N));
     // (the row's last piece may be shorter than a vector, which then starts before it)
     const T* dy = static_cast<const T*>(a.dY) + first + at.at;
     const T* h = static_cast<const T*>(a.H) + first + at.at;
@@ -138,7 +138,7 @@ __global__ __launch_bounds__(Shape::B) void backward_kernel(BackwardArgs a) {
     float gain[V][N], dgain[V][N], dbias[V][N];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        at[v] = span<TPR, N>(v, l, a.n);
+        at[v] = span<TPR, V, N>(v, l, a.n);
         load_gain<N>(a, at[v].at, gain[v]);
 #pragma unroll
         for (int i = 0; i < N; ++i) dgain[v][i] = dbias[v][i] = 0.f;
@@ -361,7 +361,7 @@ int backward_blocks(int64_t T, int64_t n, grass_dtype dt) {
 }
 
 // Rows up to which dgain and dbias are added up beside dX in one launch.
-constexpr int64_t kFewRows = 64;
+constexpr int64_t kFewRows = 128;
 
 // True where dgain and dbias are done with, false where the blocks' sums wait to be added.
 template <typename T>

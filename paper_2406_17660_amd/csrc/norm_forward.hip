@@ -84,7 +84,7 @@ __global__ __launch_bounds__(Shape::B) void forward_kernel(ForwardArgs a) {
     int64_t t0 = static_cast<int64_t>(blockIdx.x) * kRows;
     Span at[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v) at[v] = span<TPR, N>(v, l, a.n);
+    for (int v = 0; v < V; ++v) at[v] = span<TPR, V, N>(v, l, a.n);
     RowPart even, odd;
     even.load(a, t0 + group, l, at);
     float gain[V][N], bias[V][N];
