@@ -577,44 +577,47 @@ def gather_rows(G, idx, rho, out):
     return out
 
 
-def _like(t, shape, dtype):
-    """(address, leading dimension) of a matrix of that shape and dtype with contiguous rows."""
-    assert t.is_cuda and t.dtype == dtype and t.shape == shape, "matrices of one shape and dtype on the GPU"
-    ld, step = t.stride()
-    T, n = shape
-    if T > 1 and n > 0:
-        assert step == 1 or n == 1, "rows must be contiguous"
-    elif ld < n:
-        ld = n
-    return t.data_ptr(), ld
-
-
 def _vector(t, n, dtype):
-    """Address of n contiguous values, or None."""
-    if t is None:
-        return None
-    assert t.is_cuda and t.dtype == dtype and t.shape == (n,) and t.is_contiguous()
+    """Address of n contiguous values."""
+    assert t.is_cuda and t.dtype is dtype and t.shape == (n,) and t.is_contiguous()
     return t.data_ptr()
 
 
+# (A norm of few rows takes the GPU less time than a call's checks take here; these are therefore written
+# out, each value read once: 6.8 -> 5.3 us on a machine where a call into the library takes 1.5.)
 def norm_forward(X, gain, bias, eps, Y, kind=NORM_LAYER, R=None, H=None, mean=None, rstd=None):
     """Layer norm or RMS norm (kind) of the rows of X, or of X + R, which H then receives; mean and
     rstd: T floats for the backward pass, or None."""
-    shape, dtype = X.shape, X.dtype
-    pX, ldx = _like(X, shape, dtype)
-    pY, ldy = _like(Y, shape, dtype)
+    shape, dtype, f32 = X.shape, X.dtype, torch.float32
     T, n = shape
+    ldx, x = X.stride()
+    ldy, y = Y.stride()
+    assert X.is_cuda and Y.is_cuda and Y.shape == shape and Y.dtype is dtype and (x == y == 1 or n <= 1)
     pR = pH = None
     ldr = ldh = n
     if R is not None:
-        pR, ldr = _like(R, shape, dtype)
-        pH, ldh = _like(H, shape, dtype)
-    one = gain if gain is not None else bias
-    gdtype = torch.float32 if one is None else one.dtype
-    _check(lib().grass_norm_forward(kind, pX, ldx, pR, ldr, _dtype(X), T, n, _vector(gain, n, gdtype),
-                                    _vector(bias, n, gdtype), F32 if one is None else _dtype(one), eps, pH, ldh, pY, ldy,
-                                    _vector(mean, T, torch.float32), _vector(rstd, T, torch.float32), _stream()),
-           "grass_norm_forward")
+        ldr, r = R.stride()
+        ldh, h = H.stride()
+        assert R.is_cuda and H.is_cuda and R.shape == H.shape == shape and R.dtype is H.dtype is dtype and (r == h == 1 or n <= 1)
+        pR, pH = R.data_ptr(), H.data_ptr()
+    if T <= 1:
+        ldx = ldy = ldr = ldh = n
+    pgain = pbias = pmean = prstd = None
+    gdtype = f32
+    if gain is not None:
+        gdtype = gain.dtype
+        pgain = _vector(gain, n, gdtype)
+    if bias is not None:
+        gdtype = bias.dtype if gain is None else gdtype
+        pbias = _vector(bias, n, gdtype)
+    if mean is not None:
+        pmean = _vector(mean, T, f32)
+    if rstd is not None:
+        prstd = _vector(rstd, T, f32)
+    if dtype not in _DTYPES or gdtype not in _DTYPES:
+        raise TypeError(f"unsupported dtype {dtype} or {gdtype}")
+    _check(lib().grass_norm_forward(kind, X.data_ptr(), ldx, pR, ldr, _DTYPES[dtype], T, n, pgain, pbias, _DTYPES[gdtype],
+                                    eps, pH, ldh, Y.data_ptr(), ldy, pmean, prstd, _stream()), "grass_norm_forward")
     return Y
 
 
@@ -626,17 +629,36 @@ def norm_backward(dY, H, gain, mean, rstd, dX, dgain, dbias, ws, kind=NORM_LAYER
     """Backward pass of norm_forward: dX (plus dR where given), dgain and dbias (fp32, or None) from the
     rows H that were normed and the statistics that the forward pass kept."""
     shape, dtype, f32 = dY.shape, dY.dtype, torch.float32
-    pY, lddy = _like(dY, shape, dtype)
-    pH, ldh = _like(H, shape, dtype)
-    pX, lddx = _like(dX, shape, dtype)
     T, n = shape
-    pR, lddr = (None, n) if dR is None else _like(dR, shape, dtype)
-    gdtype = f32 if gain is None else gain.dtype
+    lddy, y = dY.stride()
+    ldh, h = H.stride()
+    lddx, x = dX.stride()
+    assert dY.is_cuda and H.is_cuda and dX.is_cuda and H.shape == dX.shape == shape
+    assert H.dtype is dX.dtype is dtype and (y == h == x == 1 or n <= 1)
+    pR, lddr = None, n
+    if dR is not None:
+        lddr, r = dR.stride()
+        assert dR.is_cuda and dR.shape == shape and dR.dtype is dtype and (r == 1 or n <= 1)
+        pR = dR.data_ptr()
+    if T <= 1:
+        lddy = ldh = lddx = lddr = n
+    pgain = pmean = pdgain = pdbias = None
+    gdtype = f32
+    if gain is not None:
+        gdtype = gain.dtype
+        pgain = _vector(gain, n, gdtype)
+    if mean is not None:
+        pmean = _vector(mean, T, f32)
+    if dgain is not None:
+        pdgain = _vector(dgain, n, f32)
+    if dbias is not None:
+        pdbias = _vector(dbias, n, f32)
     wp, wb = _ws(ws)
-    _check(lib().grass_norm_backward(kind, pY, lddy, pH, ldh, pR, lddr, _dtype(dY), T, n, _vector(gain, n, gdtype),
-                                     F32 if gain is None else _dtype(gain), _vector(mean, T, f32), _vector(rstd, T, f32), pX, lddx,
-                                     _vector(dgain, n, f32), _vector(dbias, n, f32), wp, wb, _stream()),
-           "grass_norm_backward")
+    if dtype not in _DTYPES or gdtype not in _DTYPES:
+        raise TypeError(f"unsupported dtype {dtype} or {gdtype}")
+    _check(lib().grass_norm_backward(kind, dY.data_ptr(), lddy, H.data_ptr(), ldh, pR, lddr, _DTYPES[dtype], T, n, pgain,
+                                     _DTYPES[gdtype], pmean, _vector(rstd, T, f32), dX.data_ptr(), lddx, pdgain, pdbias,
+                                     wp, wb, _stream()), "grass_norm_backward")
     return dX
 
 
