@@ -112,6 +112,18 @@ __device__ __forceinline__ uint32_t row_max(uint32_t x) {
     return max(x, row_rotate<1>(x));
 }
 
+// The largest of the LANES (16 or 32) consecutive lanes that hold a block, in every one of them.
+template <int LANES>
+__device__ __forceinline__ uint32_t block_max(uint32_t x) {
+    static_assert(LANES == 16 || LANES == 32, "one row of 16 lanes or two");
+    x = row_max(x);
+    if constexpr (LANES == 32) {
+        const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+        x = max(r[0], r[1]);
+    }
+    return x;
+}
+
 constexpr uint32_t kInf = 0x7F800000u;
 
 // One kind of 8-bit moment: kMan bits of mantissa, scale 2^(e - kTop).  Scaled by a further
@@ -120,15 +132,16 @@ constexpr uint32_t kInf = 0x7F800000u;
 template <int kMan, int kTop, int kBias>
 struct Code8 {
     static constexpr int kCut = 23 - kMan;
-    // what the eight lanes' values allow as a scale (all 16 lanes of the block get the same)
-    __device__ static __forceinline__ uint32_t exponent(const float (&x)[8]) {
+    // the exponent of the block's largest value from its lanes' N values each (all of them get the same)
+    template <int N>
+    __device__ static __forceinline__ uint32_t exponent(const float (&x)[N]) {
         uint32_t top = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < N; ++i) {
             const uint32_t b = __float_as_uint(x[i]) & 0x7FFFFFFFu;
             top = max(top, b < kInf ? b : 0u);
         }
-        return max(row_max(top) >> 23, 24u);
+        return max(block_max<kQBlock / N>(top) >> 23, 24u);
     }
     __device__ static __forceinline__ float scale(uint32_t e) { return __uint_as_float((e - kTop) << 23); }
     __device__ static __forceinline__ uint32_t code(float x, float inv_scale, uint32_t word) {
@@ -137,53 +150,78 @@ struct Code8 {
         const uint32_t c = ((__float_as_uint(y) & 0x7FFFFFFFu) + (word >> (32 - kCut))) >> kCut;
         return ((b & 0x7FFFFFFFu) < kInf ? c : 0x7Fu) | (b >> 31 << 7);
     }
-    // the eight lanes' codes; word: u's bits at the first of them
-    __device__ static __forceinline__ raw2_t codes(const float (&x)[8], uint32_t e, uint32_t word) {
+    // codes of N values; word: u's bits at the first of them
+    template <int N>
+    __device__ static __forceinline__ void codes(const float (&x)[N], uint32_t e, uint32_t word, uint32_t (&r)[N / 4]) {
         const float inv = __uint_as_float((254u + kTop - e) << 23);
-        raw2_t r = {0, 0};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) r[i / 4] |= code(x[i], inv, word + i * 0x9E3779B1u) << (8 * (i & 3));
-        return r;
+        for (int i = 0; i < N / 4; ++i) r[i] = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) r[i / 4] |= code(x[i], inv, word + i * 0x9E3779B1u) << (8 * (i & 3));
     }
 };
 typedef Code8<3, 7, 7> CodeM;     // e4m3
 typedef Code8<2, 14, 15> CodeV;   // e5m2
 
-template <bool kOnce>
-__device__ __forceinline__ raw2_t load_codes(const void* p, int at, int left) {
+// N codes from any byte on, four to a word.
+typedef uint32_t word_any_t __attribute__((aligned(1)));
+template <bool kOnce, int N>
+__device__ __forceinline__ void load_codes(const void* p, int at, int left, uint32_t (&r)[N / 4]) {
     const uint8_t* q = static_cast<const uint8_t*>(p) + at;
-    const raw2_any_t* whole = reinterpret_cast<const raw2_any_t*>(q);
-    if (left >= 8) return kOnce ? __builtin_nontemporal_load(whole) : *whole;
-    raw2_t r = {0, 0};
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (i < left) r[i / 4] |= static_cast<uint32_t>(q[i]) << (8 * (i & 3));
-    return r;
-}
-template <bool kOnce>
-__device__ __forceinline__ void store_codes(void* p, int at, int left, raw2_t r) {
-    uint8_t* q = static_cast<uint8_t*>(p) + at;
-    if (left >= 8) {
-        raw2_any_t* whole = reinterpret_cast<raw2_any_t*>(q);
-        if constexpr (kOnce) __builtin_nontemporal_store(r, whole);
-        else *whole = r;
+    if (left >= N) {
+        if constexpr (N == 8) {
+            const raw2_any_t* whole = reinterpret_cast<const raw2_any_t*>(q);
+            const raw2_t a = kOnce ? __builtin_nontemporal_load(whole) : *whole;
+            r[0] = a[0];
+            r[1] = a[1];
+        } else {
+            const word_any_t* whole = reinterpret_cast<const word_any_t*>(q);
+            r[0] = kOnce ? __builtin_nontemporal_load(whole) : *whole;
+        }
         return;
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < N / 4; ++i) r[i] = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (i < left) r[i / 4] |= static_cast<uint32_t>(q[i]) << (8 * (i & 3));
+}
+template <bool kOnce, int N>
+__device__ __forceinline__ void store_codes(void* p, int at, int left, const uint32_t (&r)[N / 4]) {
+    uint8_t* q = static_cast<uint8_t*>(p) + at;
+    if (left >= N) {
+        if constexpr (N == 8) {
+            const raw2_t a = {r[0], r[1]};
+            raw2_any_t* whole = reinterpret_cast<raw2_any_t*>(q);
+            if constexpr (kOnce) __builtin_nontemporal_store(a, whole);
+            else *whole = a;
+        } else {
+            word_any_t* whole = reinterpret_cast<word_any_t*>(q);
+            if constexpr (kOnce) __builtin_nontemporal_store(r[0], whole);
+            else *whole = r[0];
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
         if (i < left) q[i] = static_cast<uint8_t>(r[i / 4] >> (8 * (i & 3)));
 }
 
-// ... and 8 bits.  Every lane of the wavefront takes part in store(), those without elements too.
+// ... and 8 bits: eight at a time, or four where W is fp32, whose accesses are whole pieces then (66M values of
+// fp32 W and G: 172 us, 190 with eight; 262M of bf16: 482, with eight 419).  Every lane of the wavefront takes
+// part in store(), those without elements too.
+template <int N_>
 struct MomentsQ8 {
-    static constexpr int N = 8, V = 1;
+    static constexpr int N = N_, V = 8 / N_;
     float m[N], v[N];
     template <bool kOnce>
     __device__ __forceinline__ void load(const Chunk& c, int at, int left) {
-        const raw2_t a = load_codes<kOnce>(c.M, at, left), b = load_codes<kOnce>(c.V, at, left);
+        uint32_t a[N / 4], b[N / 4];
+        load_codes<kOnce, N>(c.M, at, left, a);
+        load_codes<kOnce, N>(c.V, at, left, b);
         const float sm = left > 0 ? c.mscale[at / kQBlock] : 0.f, sv = left > 0 ? c.vscale[at / kQBlock] : 0.f;
 #pragma unroll
-        for (int w = 0; w < 2; ++w) {
+        for (int w = 0; w < N / 4; ++w) {
             const f32x2_t m0 = __builtin_amdgcn_cvt_pk_f32_fp8(a[w], false), m1 = __builtin_amdgcn_cvt_pk_f32_fp8(a[w], true);
             const f32x2_t v0 = __builtin_amdgcn_cvt_pk_f32_bf8(b[w], false), v1 = __builtin_amdgcn_cvt_pk_f32_bf8(b[w], true);
             m[4 * w] = m0.x * sm; m[4 * w + 1] = m0.y * sm; m[4 * w + 2] = m1.x * sm; m[4 * w + 3] = m1.y * sm;
@@ -194,10 +232,12 @@ struct MomentsQ8 {
     __device__ __forceinline__ void store(const Chunk& c, int at, int left, uint32_t t) const {
         const uint32_t em = CodeM::exponent(m), ev = CodeV::exponent(v);
         const uint32_t j = static_cast<uint32_t>(at % kQBlock) * 0x9E3779B1u;
-        const raw2_t a = CodeM::codes(m, em, j + t * 0x6A09E667u), b = CodeV::codes(v, ev, j + t * 0xBB67AE85u);
+        uint32_t a[N / 4], b[N / 4];
+        CodeM::codes(m, em, j + t * 0x6A09E667u, a);
+        CodeV::codes(v, ev, j + t * 0xBB67AE85u, b);
         if (left <= 0) return;
-        store_codes<kOnce>(c.M, at, left, a);
-        store_codes<kOnce>(c.V, at, left, b);
+        store_codes<kOnce, N>(c.M, at, left, a);
+        store_codes<kOnce, N>(c.V, at, left, b);
         if (at % kQBlock == 0) {
             c.mscale[at / kQBlock] = CodeM::scale(em);
             c.vscale[at / kQBlock] = CodeV::scale(ev);
@@ -458,13 +498,13 @@ grass_status launch_adamw(const void* plan, const grass_adamw_layout& layout, fl
             const unsigned grid = static_cast<unsigned>(now);
             switch (i) {
                 case 0: adamw_kernel<float, float, MomentsF32><<<grid, kThreads, 0, s>>>(a); break;
-                case 1: adamw_kernel<float, float, MomentsQ8><<<grid, kThreads, 0, s>>>(a); break;
+                case 1: adamw_kernel<float, float, MomentsQ8<4>><<<grid, kThreads, 0, s>>>(a); break;
                 case 2: adamw_kernel<float, uint16_t, MomentsF32><<<grid, kThreads, 0, s>>>(a); break;
-                case 3: adamw_kernel<float, uint16_t, MomentsQ8><<<grid, kThreads, 0, s>>>(a); break;
+                case 3: adamw_kernel<float, uint16_t, MomentsQ8<4>><<<grid, kThreads, 0, s>>>(a); break;
                 case 4: adamw_kernel<uint16_t, float, MomentsF32><<<grid, kThreads, 0, s>>>(a); break;
-                case 5: adamw_kernel<uint16_t, float, MomentsQ8><<<grid, kThreads, 0, s>>>(a); break;
+                case 5: adamw_kernel<uint16_t, float, MomentsQ8<8>><<<grid, kThreads, 0, s>>>(a); break;
                 case 6: adamw_kernel<uint16_t, uint16_t, MomentsF32><<<grid, kThreads, 0, s>>>(a); break;
-                case 7: adamw_kernel<uint16_t, uint16_t, MomentsQ8><<<grid, kThreads, 0, s>>>(a); break;
+                case 7: adamw_kernel<uint16_t, uint16_t, MomentsQ8<8>><<<grid, kThreads, 0, s>>>(a); break;
             }
             a.chunks += now;
             left -= now;

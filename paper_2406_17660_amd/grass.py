@@ -596,6 +596,7 @@ def norm_forward(X, gain, bias, eps, Y, kind=NORM_LAYER, R=None, H=None, mean=No
     pR = pH = None
     ldr = ldh = n
     if R is not None:
+        assert H is not None, "the sum is stored"
         ldr, r = R.stride()
         ldh, h = H.stride()
         assert R.is_cuda and H.is_cuda and R.shape == H.shape == shape and R.dtype is H.dtype is dtype and (r == h == 1 or n <= 1)
