@@ -78,20 +78,21 @@ struct Row {
     }
 };
 
-// Few rows: dgain and dbias of 64 vectors of columns, whole, by one block; its wavefronts take rows in turn.
-// (That reads dY and H twice, and spares the second kernel and what goes between the two.)
+// Few rows: dgain and dbias of 16 vectors of columns, whole, by one block, whose groups of 16 lanes take
+// rows in turn.  (That reads dY and H twice, and spares the second kernel and what goes between the two.)
+constexpr int kColumnLanes = 16;
 template <typename T, int B>
 __device__ __forceinline__ void add_columns_up(const BackwardArgs& a, float* sums) {
-    constexpr int N = 16 / sizeof(T), kWaves = B / kWave;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
-    const int64_t first = static_cast<int64_t>(blockIdx.x) * kWave * N;
-    const Span at = span<kWave, 1, N>(0, lane, static_cast<int>(a.n - first < kWave * N ? a.n - first : kWave * N));
+    constexpr int N = 16 / sizeof(T), kColumns = kColumnLanes * N, kGroups = B / kColumnLanes;
+    const int group = threadIdx.x / kColumnLanes, lane = threadIdx.x % kColumnLanes;
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * kColumns;
     // (the row's last piece may be shorter than a vector, which then starts before it)
+    const Span at = span<kColumnLanes, 1, N>(0, lane, static_cast<int>(a.n - first < kColumns ? a.n - first : kColumns));
     const T* dy = static_cast<const T*>(a.dY) + first + at.at;
     const T* h = static_cast<const T*>(a.H) + first + at.at;
     float dgain[N] = {}, dbias[N] = {};
 #pragma unroll 4
-    for (int64_t t = wave; t < a.T; t += kWaves) {
+    for (int64_t t = group; t < a.T; t += kGroups) {
         Raw<T, N> y, x;
         y.load(dy + t * a.lddy);
         x.load(h + t * a.ldh);
@@ -109,12 +110,12 @@ __device__ __forceinline__ void add_columns_up(const BackwardArgs& a, float* sum
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < N; ++i)
-            if (i >= at.skip) sums[wave * kWave * N + lane * N + i - at.skip] = q ? dbias[i] : dgain[i];
+            if (i >= at.skip) sums[group * kColumns + lane * N + i - at.skip] = q ? dbias[i] : dgain[i];
         __syncthreads();
-        for (int c = threadIdx.x; c < kWave * N; c += B) {
+        for (int c = threadIdx.x; c < kColumns; c += B) {
             float s = sums[c];
 #pragma unroll
-            for (int w = 1; w < kWaves; ++w) s += sums[w * kWave * N + c];
+            for (int g = 1; g < kGroups; ++g) s += sums[g * kColumns + c];
             if (first + c < a.n) out[first + c] = s;
         }
     }
@@ -360,8 +361,10 @@ int backward_blocks(int64_t T, int64_t n, grass_dtype dt) {
     return static_cast<int>(want < kUnits ? want : kUnits);
 }
 
-// Rows up to which dgain and dbias are added up beside dX in one launch.
-constexpr int64_t kFewRows = 128;
+// Rows up to which dgain and dbias are added up beside dX in one launch.  180 rows, one launch and two: 4096
+// bf16 8.3 and 10.8 us, 7162 fp32 8.5 and 16.4; 546 rows: 9.3 and 12.6, 17.7 and 22.7, 233 bf16 9.4 and 10.8;
+// 1000 rows: 13.9 and 14.1, 28.3 and 29.8, 14.1 and 10.8.
+constexpr int64_t kFewRows = 768;
 
 // True where dgain and dbias are done with, false where the blocks' sums wait to be added.
 template <typename T>
@@ -399,7 +402,7 @@ bool launch(BackwardArgs a, hipStream_t s) {
         return false;
     }
     a.part = nullptr;
-    constexpr int kColumns = kWave * 16 / static_cast<int>(sizeof(T));
+    constexpr int kColumns = kColumnLanes * 16 / static_cast<int>(sizeof(T));
     const unsigned columns = static_cast<unsigned>((a.n + kColumns - 1) / kColumns);
     if (a.dX != a.dY && a.dX != a.H) {
         run(columns, rows);
