@@ -392,7 +392,7 @@ __device__ __forceinline__ void write_norm(double s, float max_norm, float* out)
     out[1] = s <= 1.7976931348623157e308 ? static_cast<float>(factor) : __uint_as_float(0x7FC00000u);
 }
 
-// kOnce: more gradients than the last-level cache holds, read with the streaming hint where accesses are whole
+// kOnce: from kStreamed bytes on, read with the streaming hint where accesses are whole
 // pieces (262M bf16 values 88.5 -> 83.4 us; it costs where they are not: 7M values in 300 tensors 8.8 -> 9.6).
 template <bool kOnce>
 __global__ __launch_bounds__(kThreads) void grad_squares_kernel(const Chunk* __restrict__ chunks, int64_t count, double* part) {
@@ -528,7 +528,7 @@ grass_status launch_grad_norm(const void* plan, const grass_adamw_layout& layout
     double bytes = 0;
     for (int i = 0; i < GRASS_ADAMW_GROUPS; ++i)
         bytes += static_cast<double>(layout.chunks[i]) * kChunk * (gradient_of(i) == GRASS_F32 ? 4 : 2);
-    (bytes > kLastLevel ? grad_squares_kernel<true> : grad_squares_kernel<false>)
+    (bytes > kStreamed ? grad_squares_kernel<true> : grad_squares_kernel<false>)
         <<<static_cast<unsigned>(blocks), kThreads, 0, s>>>(static_cast<const Chunk*>(plan), chunks_in(layout), part);
     grad_norm_kernel<<<1, kThreads, 0, s>>>(part, blocks, max_norm, out);
     return launch_status();

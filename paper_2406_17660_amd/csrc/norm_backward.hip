@@ -381,7 +381,7 @@ bool launch(BackwardArgs a, hipStream_t s) {
     const auto on16 = [](const void* p, int64_t ld) { return aligned_to(p, 16) && ld * sizeof(T) % 16 == 0; };
     const bool window = a.n * sizeof(T) % 16 == 0 && on16(a.dY, a.lddy) && on16(a.H, a.ldh) && on16(a.dX, a.lddx) &&
                         (!a.dR || on16(a.dR, a.lddr));
-    const bool once = static_cast<double>(a.T) * a.n * sizeof(T) * (a.dR ? 4 : 3) > kLastLevel;
+    const bool once = static_cast<double>(a.T) * a.n * sizeof(T) * (a.dR ? 4 : 3) > kStreamed;
     const auto run = [&](unsigned column_blocks, unsigned row_blocks) {
         a.column_blocks = column_blocks;
         by_shape<T>(a.n, [&](auto shape) {

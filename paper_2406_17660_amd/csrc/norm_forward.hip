@@ -248,7 +248,7 @@ __global__ __launch_bounds__(kWide) void forward_wide_kernel(ForwardArgs a) {
     }
 }
 
-// Blocks for so many groups of rows.  What stays in the last-level cache: two per compute unit, which walk
+// Blocks for so many groups of rows.  Short of kStreamed bytes two per compute unit, which walk
 // the rest.  Beyond that more of them, so that the memory sees rows in order as they start and end: all of
 // them with a residual branch, a fourth without.  131072 x 4096 bf16 with it: 708 us so, 762 with two per
 // unit; without: 355 so, 413 with two, 430 with all.  131072 x 1024 without: 91, 97, 116.
@@ -266,7 +266,7 @@ void launch(const ForwardArgs& a, hipStream_t s) {
     const auto on16 = [](const void* p, int64_t ld) { return aligned_to(p, 16) && ld * sizeof(T) % 16 == 0; };
     const bool window = a.n * sizeof(T) % 16 == 0 && on16(a.X, a.ldx) && on16(a.Y, a.ldy) &&
                         (!a.R || (on16(a.R, a.ldr) && on16(a.H, a.ldh)));
-    const bool once = static_cast<double>(a.T) * a.n * sizeof(T) * (a.R ? 4 : 2) > kLastLevel;
+    const bool once = static_cast<double>(a.T) * a.n * sizeof(T) * (a.R ? 4 : 2) > kStreamed;
     by_shape<T>(a.n, [&](auto shape) {
         typedef decltype(shape) S;
         constexpr int64_t kRows = S::B / S::TPR;
