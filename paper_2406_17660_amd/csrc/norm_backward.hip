@@ -211,18 +211,30 @@ __global__ __launch_bounds__(Shape::B) void backward_kernel(BackwardArgs a) {
         if (q == 1 && !a.want_bias) break;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            __syncthreads();
-            // a column's sums stand where its own thread's element would without the shift at the row's end
+            const float(&own)[N] = q ? dbias[v] : dgain[v];
+            const int skip = at[v].skip;
+            if constexpr (kRows == 1) {  // the thread has seen all of the block's rows
+                float* p = part + static_cast<int64_t>(q) * a.n + at[v].at;
+                Raw<float, N> r;
+                r.set(own);
+                if (skip == 0) r.store(p);
+                else
 #pragma unroll
-            for (int i = 0; i < N; ++i)
-                if (kWindow || i >= at[v].skip)
-                    sums[(group * TPR + l) * N + i - (kWindow ? 0 : at[v].skip)] = q ? dbias[v][i] : dgain[v][i];
-            __syncthreads();
-            for (int c = threadIdx.x; c < TPR * N; c += B) {
-                float s = sums[c];
+                    for (int i = 0; i < N; ++i)
+                        if (i >= skip) p[i] = own[i];
+            } else {
+                __syncthreads();
+                // a column's sums stand where its own thread's element would without the shift at the row's end
 #pragma unroll
-                for (int r = 1; r < kRows; ++r) s += sums[r * TPR * N + c];
-                if (v * TPR * N + c < a.n) part[static_cast<int64_t>(q) * a.n + v * TPR * N + c] = s;
+                for (int i = 0; i < N; ++i)
+                    if (kWindow || i >= skip) sums[(group * TPR + l) * N + i - (kWindow ? 0 : skip)] = own[i];
+                __syncthreads();
+                for (int c = threadIdx.x; c < TPR * N; c += B) {
+                    float s = sums[c];
+#pragma unroll
+                    for (int r = 1; r < kRows; ++r) s += sums[r * TPR * N + c];
+                    if (v * TPR * N + c < a.n) part[static_cast<int64_t>(q) * a.n + v * TPR * N + c] = s;
+                }
             }
         }
     }
