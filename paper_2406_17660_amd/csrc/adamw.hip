@@ -400,10 +400,12 @@ __global__ __launch_bounds__(kThreads) void grad_squares_kernel(const Chunk* __r
     if (threadIdx.x == 0) part[blockIdx.x] = s;
 }
 
-__global__ __launch_bounds__(kThreads) void grad_norm_kernel(const double* __restrict__ part, int count, float max_norm, float* out) {
+// (1024 threads: two of the most sums each, 4.2 us with 256 threads)
+constexpr int kJoinThreads = 1024;
+__global__ __launch_bounds__(kJoinThreads) void grad_norm_kernel(const double* __restrict__ part, int count, float max_norm, float* out) {
     double s = 0.0;
-    for (int k = threadIdx.x; k < count; k += kThreads) s += part[k];
-    s = block_sum<kThreads>(s);
+    for (int k = threadIdx.x; k < count; k += kJoinThreads) s += part[k];
+    s = block_sum<kJoinThreads>(s);
     if (threadIdx.x == 0) write_norm(s, max_norm, out);
 }
 
@@ -530,7 +532,7 @@ grass_status launch_grad_norm(const void* plan, const grass_adamw_layout& layout
         bytes += static_cast<double>(layout.chunks[i]) * kChunk * (gradient_of(i) == GRASS_F32 ? 4 : 2);
     (bytes > kStreamed ? grad_squares_kernel<true> : grad_squares_kernel<false>)
         <<<static_cast<unsigned>(blocks), kThreads, 0, s>>>(static_cast<const Chunk*>(plan), chunks_in(layout), part);
-    grad_norm_kernel<<<1, kThreads, 0, s>>>(part, blocks, max_norm, out);
+    grad_norm_kernel<<<1, kJoinThreads, 0, s>>>(part, blocks, max_norm, out);
     return launch_status();
 }
 
