@@ -1,6 +1,6 @@
 /*
- * grass.h - C ABI of the GRASS structured-sparse gradient step for one linear layer
- *           on one AMD MI355X (gfx950).
+ * grass.h - C ABI of the GRASS structured-sparse gradient step for one linear layer, and of the norms
+ *           and the AdamW step around it, on one AMD MI355X (gfx950).
  *
  * Notation (paper, Sections 2 and 3.1): a linear layer has weight W (m x n), input
  * activations X (T x n) and output gradient dY (T x m), T being the token batch
