@@ -20,8 +20,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2_t));
 }
 
-// The elements as they lie in memory.  load_once, store_once: the streaming hint, for what is not
-// read again soon.
+// The elements as they lie in memory.  kOnce: the streaming hint, for what is not read again soon.
 template <typename T, int N>
 struct Raw {
     static constexpr bool kHalf = sizeof(T) == 2;
@@ -63,9 +62,7 @@ struct Raw {
         }
     }
     __device__ __forceinline__ void load(const T* p) { load_as<false>(p); }
-    __device__ __forceinline__ void load_once(const T* p) { load_as<true>(p); }
     __device__ __forceinline__ void store(T* p) const { store_as<false>(p); }
-    __device__ __forceinline__ void store_once(T* p) const { store_as<true>(p); }
     __device__ __forceinline__ void zero() {
 #pragma unroll
         for (int k = 0; k < kWords; ++k) w[k] = 0;
@@ -189,7 +186,7 @@ struct RowSum {
 // share: every vector is read and written whole.  The one that would end behind the row is the row's
 // last N values instead, whose first `skip` are the thread before's too: both compute and write the
 // same there, and sums leave them out here.  A vector without values of its own (skip = N) is another
-// copy of the row's last.  With V > 1 vectors per thread the row fills the first half of them (see by_shape).
+// copy of the row's last.  With V > 1 vectors per thread a row fills the first half of them: by_shape chooses V so.
 struct Span {
     int at, skip;
 };

@@ -146,7 +146,7 @@ __global__ __launch_bounds__(Shape::B) void backward_kernel(BackwardArgs a) {
     }
     const int64_t step = static_cast<int64_t>(blocks) * kRows;
     int64_t t0 = static_cast<int64_t>(block) * kRows;
-    const auto work = [&](const RowPart& row, int64_t t) {
+    const auto work = [&](RowPart& row, int64_t t) {
         const bool there = kRows == 1 || t < a.T;
         const float mean = a.centre ? row.mean : 0.f, rstd = row.rstd;
         float s[2] = {0.f, 0.f};
@@ -164,7 +164,14 @@ __global__ __launch_bounds__(Shape::B) void backward_kernel(BackwardArgs a) {
                 dbias[v][i] += d;
             }
         }
-        // (behind row_sum all threads of the row have what they read of it, so that dX may lie over it)
+        // Behind row_sum all threads of the row have what they read of it, so that dX may lie over it: dY and H,
+        // which are in the sums, and dR, which is waited for here where two threads write the same elements.
+        if constexpr (kAdd && !kWindow && TPR > kWave) {
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(row.b[v].w[i]));
+        }
         row_sum(s);
         const float c0 = s[0] * inv_n, c1 = a.centre ? s[1] * inv_n : 0.f;
         T* dx = static_cast<T*>(a.dX) + t * a.lddx;

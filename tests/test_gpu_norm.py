@@ -211,6 +211,25 @@ def test_outputs_in_place(n):
         assert all(torch.equal(x, y) for x, y in zip(got, want))
 
 
+@pytest.mark.parametrize("T,n,dtype", [(2000, 1293, torch.float32), (1500, 2055, torch.bfloat16), (900, 4097, torch.bfloat16),
+                                       (1200, 8193, torch.bfloat16), (500, 9001, torch.float32)])
+def test_outputs_in_place_where_rows_start_anywhere(T, n, dtype):
+    """Rows that several wavefronts share and whose last vector lies over the one before: dX over each of its
+    inputs, and H and Y over theirs, give what separate arrays give."""
+    gain = draw(n, 1, torch.float32, 0.2, 1.0)
+    X, R, dY, dR = (draw((T, n), k, dtype) for k in (3, 4, 5, 7))
+    H, Y, mean, rstd = torch.empty_like(X), torch.empty_like(X), nan((T,)), nan((T,))
+    grass.norm_forward(X, gain, None, EPS, Y, R=R, H=H, mean=mean, rstd=rstd)
+    a, b = X.clone(), R.clone()
+    grass.norm_forward(a, gain, None, EPS, a, R=b, H=b)
+    assert torch.equal(a, Y) and torch.equal(b, H)
+    want = gpu_backward(dY, H, gain, mean, rstd, "layer", dR)
+    for which in range(3):
+        a = [dY.clone(), H.clone(), dR.clone()]
+        got = gpu_backward(a[0], a[1], gain, mean, rstd, "layer", a[2], dX=a[which])
+        assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
 @pytest.mark.parametrize("n", [9, 1024, 4097, 17000])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_values_that_are_not_finite_stay_in_their_row(n, dtype):
