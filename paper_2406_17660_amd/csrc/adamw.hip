@@ -4,9 +4,9 @@
 // tensors into chunks of 2048 elements and holds for each the addresses where it starts, so that a
 // workgroup finds its work with one 64-byte load whatever the number and sizes of the tensors;
 // chunks of one combination of types lie together and take one launch.  A thread handles eight consecutive
-// elements, or twice four where an fp32 array is among those written; the 16 or 32 lanes that hold a block of 128
+// elements, or four (twice, beside 8-bit moments) where an fp32 array is among those written; the 16 or 32 lanes that hold a block of 128
 // lie in one row of a wavefront or two, which exchange values without LDS.  Measured on large tensors: 6.0 TB/s
-// with fp32 moments (65.6M values of bf16 W and G: 243 us), 6.3 to 6.4 with 8-bit ones (262M: 415 to 422 us), 6.5
+// with fp32 moments (65.6M values of bf16 W and G: 240 us), 6.3 to 6.4 with 8-bit ones (262M: 415 to 422 us), 6.5
 // for the norm (262M bf16 gradients: 81 us); a step of 65 tensors of 4096 takes its kernel 3.5 us.
 #include "adam.hpp"
 #include "elem.hpp"
@@ -14,8 +14,8 @@
 namespace grass {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kChunk = kThreads * 8;
+constexpr int kChunk = 2048;
+constexpr int kThreads = kChunk / 8;  // of the norm's kernels
 constexpr int kQBlock = 128;  // elements that share a scale
 
 // What of a chunk starts on 16 bytes: W, G, M and V; G.
@@ -65,9 +65,10 @@ struct StepArgs {
 };
 
 // Moments of N consecutive elements of a thread, V times over a chunk.  fp32: four, so that a wavefront's
-// access is one piece of memory ...
+// access is one piece of memory, and no more, in workgroups of 512 (65.6M values 236 to 242 us, with
+// twice four in 256 244 to 246) ...
 struct MomentsF32 {
-    static constexpr int N = 4, V = 2;
+    static constexpr int N = 4, V = 1;
     float m[N], v[N];
     template <bool kOnce>
     __device__ __forceinline__ void load(const Chunk& c, int at, int left) {
@@ -247,6 +248,9 @@ struct MomentsQ8 {
     }
 };
 
+template <typename Moments>
+constexpr int kStepThreads = kChunk / (Moments::N * Moments::V);
+
 template <bool kOnce, typename W, typename G, typename Moments>
 __device__ __forceinline__ void step_chunk(const Chunk& c, const AdamParams& p, uint32_t t, float grad_scale) {
     constexpr int N = Moments::N, V = Moments::V;
@@ -255,7 +259,7 @@ __device__ __forceinline__ void step_chunk(const Chunk& c, const AdamParams& p, 
     Moments s[V];
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-        const int at = (k * kThreads + threadIdx.x) * N, left = c.elems - at;
+        const int at = (k * kStepThreads<Moments> + threadIdx.x) * N, left = c.elems - at;
         const W* pw = static_cast<const W*>(c.W) + at;
         const G* pg = static_cast<const G*>(c.G) + at;
         if (left >= N) {
@@ -270,7 +274,7 @@ __device__ __forceinline__ void step_chunk(const Chunk& c, const AdamParams& p, 
     const float keep = 1.0f - p.lr * c.weight_decay;
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-        const int at = (k * kThreads + threadIdx.x) * N, left = c.elems - at;
+        const int at = (k * kStepThreads<Moments> + threadIdx.x) * N, left = c.elems - at;
         float out[N];
 #pragma unroll
         for (int i = 0; i < N; ++i) {
@@ -298,7 +302,7 @@ __device__ __forceinline__ void step_chunk(const Chunk& c, const AdamParams& p, 
 // One chunk per workgroup.  The streaming hint only where every access is one whole piece: lines that two
 // lanes share are then read twice.
 template <typename W, typename G, typename Moments>
-__global__ __launch_bounds__(kThreads) void adamw_kernel(StepArgs a) {
+__global__ __launch_bounds__(kStepThreads<Moments>) void adamw_kernel(StepArgs a) {
     const Chunk c = a.chunks[blockIdx.x];
     const AdamParams p = resolve(a.adam);
     const uint32_t t = p.step_scalars ? static_cast<uint32_t>(p.step_scalars[3]) : a.t;
@@ -500,17 +504,21 @@ grass_status launch_adamw(const void* plan, const grass_adamw_layout& layout, fl
     for (int i = 0; i < kStepGroups; ++i) {
         // a grid has fewer than 2^32 threads
         for (int64_t left = layout.chunks[i]; left > 0;) {
-            const int64_t now = left < (int64_t{1} << 23) ? left : int64_t{1} << 23;
+            const int64_t now = left < (int64_t{1} << 22) ? left : int64_t{1} << 22;
             const unsigned grid = static_cast<unsigned>(now);
+            const auto go = [&](auto w, auto g, auto moments) {
+                typedef decltype(moments) Moments;
+                adamw_kernel<decltype(w), decltype(g), Moments><<<grid, kStepThreads<Moments>, 0, s>>>(a);
+            };
             switch (i) {
-                case 0: adamw_kernel<float, float, MomentsF32><<<grid, kThreads, 0, s>>>(a); break;
-                case 1: adamw_kernel<float, float, MomentsQ8<4>><<<grid, kThreads, 0, s>>>(a); break;
-                case 2: adamw_kernel<float, uint16_t, MomentsF32><<<grid, kThreads, 0, s>>>(a); break;
-                case 3: adamw_kernel<float, uint16_t, MomentsQ8<4>><<<grid, kThreads, 0, s>>>(a); break;
-                case 4: adamw_kernel<uint16_t, float, MomentsF32><<<grid, kThreads, 0, s>>>(a); break;
-                case 5: adamw_kernel<uint16_t, float, MomentsQ8<8>><<<grid, kThreads, 0, s>>>(a); break;
-                case 6: adamw_kernel<uint16_t, uint16_t, MomentsF32><<<grid, kThreads, 0, s>>>(a); break;
-                case 7: adamw_kernel<uint16_t, uint16_t, MomentsQ8<8>><<<grid, kThreads, 0, s>>>(a); break;
+                case 0: go(float{}, float{}, MomentsF32{}); break;
+                case 1: go(float{}, float{}, MomentsQ8<4>{}); break;
+                case 2: go(float{}, uint16_t{}, MomentsF32{}); break;
+                case 3: go(float{}, uint16_t{}, MomentsQ8<4>{}); break;
+                case 4: go(uint16_t{}, float{}, MomentsF32{}); break;
+                case 5: go(uint16_t{}, float{}, MomentsQ8<8>{}); break;
+                case 6: go(uint16_t{}, uint16_t{}, MomentsF32{}); break;
+                case 7: go(uint16_t{}, uint16_t{}, MomentsQ8<8>{}); break;
             }
             a.chunks += now;
             left -= now;
