@@ -56,7 +56,8 @@ class AdamW:
     """AdamW over (weight, gradient) pairs whose tensors stay where they are.  moments: "f32", or "q8" for
     8-bit moments of the tensors of at least `least_q8` elements (small ones, gains above all, keep
     fp32: they cost nothing).  weight_decay applies to matrices.  max_norm: the gradients' global
-    norm is clipped to it, and a step whose gradients are not finite is skipped."""
+    norm is clipped to it, and a step whose
+    gradients are not finite changes nothing (t counts it all the same)."""
 
     def __init__(self, parameters, adam=None, weight_decay=0.0, moments="f32", least_q8=4096, max_norm=None):
         assert moments in ("f32", "q8")
