@@ -132,21 +132,23 @@ __device__ __forceinline__ float dpp(float x) {
     return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), kCtrl, 0xF, 0xF, true));
 }
 
-// Sum over the LANES (16 or 64) consecutive lanes that share a row; each of them gets it, bit for bit the
+// Sum over the LANES (16, 32 or 64) consecutive lanes that share a row; each of them gets it, bit for bit the
 // same.  Exchanges inside rows of 16 lanes are part of the addition; rows of 16 and halves of the
 // wavefront are swapped between two copies.
 template <int LANES>
 __device__ __forceinline__ float sum_lanes(float v) {
-    static_assert(LANES == 16 || LANES == 64, "rows of 16 lanes or whole wavefronts");
+    static_assert(LANES == 16 || LANES == 32 || LANES == 64, "whole rows of 16 lanes");
     v += dpp<0xB1>(v);   // lanes 1 0 3 2 of each four
     v += dpp<0x4E>(v);   // lanes 2 3 0 1
     v += dpp<0x141>(v);  // mirrored in each eight
     v += dpp<0x140>(v);  // mirrored in each sixteen
-    if constexpr (LANES == 64) {
+    if constexpr (LANES >= 32) {
         const uint32_t a = __float_as_uint(v);
         const auto r = __builtin_amdgcn_permlane16_swap(a, a, false, false);
-        const float s = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-        const uint32_t b = __float_as_uint(s);
+        v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    if constexpr (LANES == 64) {
+        const uint32_t b = __float_as_uint(v);
         const auto h = __builtin_amdgcn_permlane32_swap(b, b, false, false);
         v = __uint_as_float(h[0]) + __uint_as_float(h[1]);
     }
@@ -186,36 +188,45 @@ struct RowSum {
 // share: every vector is read and written whole.  The one that would end behind the row is the row's
 // last N values instead, whose first `skip` are the thread before's too: both compute and write the
 // same there, and sums leave them out here.  A vector without values of its own (skip = N) is another
-// copy of the row's last.  With V > 1 vectors per thread a row fills the first half of them: by_shape chooses V so.
+// copy of the row's last.  The first kFull vectors of every thread lie inside the row whatever n is.
 struct Span {
     int at, skip;
 };
-template <int TPR, int V, int N>
+template <int TPR, int kFull, int N>
 __device__ __forceinline__ Span span(int v, int lane, int n) {
     const int c = (v * TPR + lane) * N;
-    if (v < V / 2 || c + N <= n) return {c, 0};
+    if (v < kFull || c + N <= n) return {c, 0};
     return {n - N, c < n ? c - (n - N) : N};
 }
 
-// Threads that share a row, each with V vectors of 16 bytes, in blocks of 512.
-template <int TPR_, int V_>
+// Threads that share a row, each with V vectors of 16 bytes of which the row fills kFull, in blocks of 512.
+template <int TPR_, int V_, int kFull_>
 struct RowShape {
-    static constexpr int TPR = TPR_, V = V_, B = 512;
+    static constexpr int TPR = TPR_, V = V_, kFull = kFull_, B = 512;
 };
 constexpr int kWidestRow = 16384;  // values of a row that stay in registers
 // The shape for a row of n values, as a call of f with it.  Two vectors per thread, so that a workgroup
-// has 16 KB of each array under way; more for the widest rows, one for the narrowest.
+// has 16 KB of each array under way, or three where two of twice as many threads would leave a quarter of them and
+// more without work; more for the widest rows, one for the narrowest.
 template <typename T, typename F>
 void by_shape(int64_t n, F&& f) {
     const int64_t vectors = (n * static_cast<int64_t>(sizeof(T)) + 15) / 16;
-    if (vectors <= 16) f(RowShape<16, 1>{});
-    else if (vectors <= 64) f(RowShape<64, 1>{});
-    else if (vectors <= 128) f(RowShape<64, 2>{});
-    else if (vectors <= 256) f(RowShape<128, 2>{});
-    else if (vectors <= 512) f(RowShape<256, 2>{});
-    else if (vectors <= 1024) f(RowShape<512, 2>{});
-    else if (vectors <= 2048) f(RowShape<512, 4>{});
-    else if constexpr (sizeof(T) == 4) f(RowShape<512, 8>{});
+    if (vectors <= 16) f(RowShape<16, 1, 0>{});
+    else if (vectors <= 32) f(RowShape<32, 1, 0>{});
+    else if (vectors <= 64) f(RowShape<64, 1, 0>{});
+    else if (vectors <= 128) f(RowShape<64, 2, 1>{});
+    else if (vectors <= 192) f(RowShape<64, 3, 2>{});
+    else if (vectors <= 256) f(RowShape<128, 2, 1>{});
+    else if (vectors <= 384) f(RowShape<128, 3, 2>{});
+    else if (vectors <= 512) f(RowShape<256, 2, 1>{});
+    else if (vectors <= 768) f(RowShape<256, 3, 2>{});
+    else if (vectors <= 1024) f(RowShape<512, 2, 1>{});
+    else if (vectors <= 1536) f(RowShape<512, 3, 2>{});
+    else if (vectors <= 2048) f(RowShape<512, 4, 3>{});
+    else if constexpr (sizeof(T) == 4) {
+        if (vectors <= 3072) f(RowShape<512, 6, 4>{});
+        else f(RowShape<512, 8, 6>{});
+    }
 }
 template <typename T>
 bool in_registers(int64_t n) { return n >= static_cast<int64_t>(16 / sizeof(T)) && n <= kWidestRow; }

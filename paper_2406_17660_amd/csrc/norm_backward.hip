@@ -88,7 +88,7 @@ __device__ __forceinline__ void add_columns_up(const BackwardArgs& a, float* sum
     const int group = threadIdx.x / kColumnLanes, lane = threadIdx.x % kColumnLanes;
     const int64_t first = static_cast<int64_t>(blockIdx.x) * kColumns;
     // (the row's last piece may be shorter than a vector, which then starts before it)
-    const Span at = span<kColumnLanes, 1, N>(0, lane, static_cast<int>(a.n - first < kColumns ? a.n - first : kColumns));
+    const Span at = span<kColumnLanes, 0, N>(0, lane, static_cast<int>(a.n - first < kColumns ? a.n - first : kColumns));
     const T* dy = static_cast<const T*>(a.dY) + first + at.at;
     const T* h = static_cast<const T*>(a.H) + first + at.at;
     float dgain[N] = {}, dbias[N] = {};
@@ -140,7 +140,7 @@ __global__ __launch_bounds__(Shape::B) void backward_kernel(BackwardArgs a) {
     float gain[V][N], dgain[V][N], dbias[V][N];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        at[v] = span<TPR, V, N>(v, l, a.n);
+        at[v] = span<TPR, Shape::kFull, N>(v, l, a.n);
         load_gain<N>(a, at[v].at, gain[v]);
 #pragma unroll
         for (int i = 0; i < N; ++i) dgain[v][i] = dbias[v][i] = 0.f;
@@ -194,7 +194,7 @@ __global__ __launch_bounds__(Shape::B) void backward_kernel(BackwardArgs a) {
         }
     };
     // (the same number of turns for every thread: they meet at the barriers of row_sum)
-    if constexpr (V <= 2) {
+    if constexpr (V <= 3) {
         RowPart even, odd;
         even.load(a, t0 + group, l, at);
         for (;; t0 += 2 * step) {

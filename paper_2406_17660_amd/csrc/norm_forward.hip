@@ -84,7 +84,7 @@ __global__ __launch_bounds__(Shape::B) void forward_kernel(ForwardArgs a) {
     int64_t t0 = static_cast<int64_t>(blockIdx.x) * kRows;
     Span at[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v) at[v] = span<TPR, V, N>(v, l, a.n);
+    for (int v = 0; v < V; ++v) at[v] = span<TPR, Shape::kFull, N>(v, l, a.n);
     RowPart even, odd;
     even.load(a, t0 + group, l, at);
     float gain[V][N], bias[V][N];
@@ -248,13 +248,16 @@ __global__ __launch_bounds__(kWide) void forward_wide_kernel(ForwardArgs a) {
     }
 }
 
-// Blocks for so many groups of rows.  Short of kStreamed bytes two per compute unit, which walk
-// the rest.  Beyond that more of them, so that the memory sees rows in order as they start and end: all of
-// them with a residual branch, a fourth without.  131072 x 4096 bf16 with it: 708 us so, 762 with two per
-// unit; without: 355 so, 413 with two, 430 with all.  131072 x 1024 without: 91, 97, 116.
-int64_t forward_blocks(int64_t groups, bool once, bool add) {
-    const int64_t some = 2 * kUnits, more = once ? (add ? groups : groups / 4) : some;
-    return groups < some ? groups : more > some ? more : some;
+// Blocks for so many groups of rows.  Short of kStreamed bytes two per compute unit, which walk the rest; from there
+// on whole multiples of that, for 16 turns or more (a few blocks beyond it would be a round of their own), or, where
+// what a block starts with (gain, bias, the first row's way) is small against a turn, one for two turns.  TB/s, means over
+// twenty widths from 200 to 16000 (240 MB to 2 GB), two per unit / 16 turns / 2 turns: bf16 without R 5.07 / 5.06 / 4.51, with R 5.13 /
+// 5.08 / 5.26, fp32 5.38 / 5.31 / 5.47; this rule 5.14, 5.33 and 5.46.
+int64_t forward_blocks(int64_t groups, bool once, bool two_turns) {
+    const int64_t some = 2 * kUnits;
+    if (groups < some || !once) return groups < some ? groups : some;
+    const int64_t more = two_turns ? groups / 2 : groups / (16 * some) * some;
+    return more > some ? more : some;
 }
 
 template <typename T>
@@ -270,8 +273,9 @@ void launch(const ForwardArgs& a, hipStream_t s) {
     by_shape<T>(a.n, [&](auto shape) {
         typedef decltype(shape) S;
         constexpr int64_t kRows = S::B / S::TPR;
+        const bool two_turns = sizeof(T) == 4 || (a.R && (window || S::TPR < kWave));
         // (a grid has fewer than 2^32 threads)
-        const int64_t blocks = forward_blocks((a.T + kRows - 1) / kRows, once, a.R != nullptr);
+        const int64_t blocks = forward_blocks((a.T + kRows - 1) / kRows, once, two_turns);
         const unsigned grid = static_cast<unsigned>(blocks < kMostBlocks ? blocks : kMostBlocks);
         const auto go = [&](auto win, auto add, auto stream) {
             forward_kernel<T, S, decltype(win)::value, decltype(add)::value, decltype(stream)::value><<<grid, S::B, 0, s>>>(a);
