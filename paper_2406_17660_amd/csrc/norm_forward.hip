@@ -2,7 +2,7 @@
 //
 // Bound by memory: X (and R) are read once and Y (and H) are written once.  A row stays in the registers of
 // the threads that share it from its sums to its outputs; gain and bias stay there for all rows that a
-// workgroup takes.  Measured: 131072 x 4096 bf16 with R 700 to 722 us (6.0 to 6.1 TB/s); one row of 4096 2.9 us.
+// workgroup takes.  Measured: 131072 x 4096 bf16 with R 716 to 726 us (5.9 to 6.0 TB/s); one row of 4096 2.9 us.
 #include <type_traits>
 
 #include "elem.hpp"
