@@ -504,10 +504,12 @@ grass_status grass_norm_backward(grass_norm kind, const void* dY, int64_t lddy, 
  * the update and are then stored: x / scale becomes the multiple floor(x / step + u) of the type's
  * step at x, where u, from [0, 1), is the top 20 (M) or 21 (V) bits of the 32-bit word
  * j * 0x9E3779B1 + t * c, j the element's place in its block and c = 0x6A09E667 (M) or
- * 0xBB67AE85 (V).  Over the steps u takes every part of [0, 1) alike, so what one step's rounding
+ * 0xBB67AE85 (V); a V that is not zero becomes one step at least.  Over the steps u takes every part of [0, 1) alike, so what one step's rounding
  * takes another gives back: rounded to the nearest value, V would stop following a gradient that
  * changes it by less than an eighth a step, which is every gradient at b2 = 0.999.  A moment that is not finite is
- * stored as NaN; the other elements of its block are not affected.  A block of zeros (state at the
+ * stored as NaN; the other elements of its block are not affected.  The smallest V of a block is 2^-30 of the
+ * power of two at its largest, so an element whose gradients stay below some 1/30000 of the block's largest
+ * takes steps that are too short, in proportion; none takes one that is too long.  A block of zeros (state at the
  * start: all codes zero, scales of any finite value) is exact.
  *
  * The tensors are laid out once into a plan, which the caller copies to device memory and passes to

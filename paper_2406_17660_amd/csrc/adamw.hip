@@ -132,7 +132,10 @@ constexpr uint32_t kInf = 0x7F800000u;
 // One kind of 8-bit moment: kMan bits of mantissa, scale 2^(e - kTop).  Scaled by a further
 // 2^(bias - 127) the type's numbers, subnormal ones too, are the fp32 numbers whose bits are the code
 // followed by zeros; so a value becomes a code by cutting its bits after adding u's bits to them.
-template <int kMan, int kTop, int kBias>
+// kLeast: the least code of a value that is not zero.  1 for V: what lies below its block's smallest code
+// would be cut to zero on most steps, while M's own cut leaves some of M, and a step that then divides M by
+// the root of nothing but its own gradient is thousands of lr long.
+template <int kMan, int kTop, int kBias, uint32_t kLeast>
 struct Code8 {
     static constexpr int kCut = 23 - kMan;
     // the exponent of the block's largest value from its lanes' N values each (all of them get the same)
@@ -150,7 +153,8 @@ struct Code8 {
     __device__ static __forceinline__ uint32_t code(float x, float inv_scale, uint32_t word) {
         const float y = (x * inv_scale) * __uint_as_float(kBias << 23);
         const uint32_t b = __float_as_uint(x);
-        const uint32_t c = ((__float_as_uint(y) & 0x7FFFFFFFu) + (word >> (32 - kCut))) >> kCut;
+        const uint32_t cut = ((__float_as_uint(y) & 0x7FFFFFFFu) + (word >> (32 - kCut))) >> kCut;
+        const uint32_t c = kLeast ? max(cut, min(b & 0x7FFFFFFFu, kLeast)) : cut;
         return ((b & 0x7FFFFFFFu) < kInf ? c : 0x7Fu) | (b >> 31 << 7);
     }
     // codes of N values; word: u's bits at the first of them
@@ -163,8 +167,8 @@ struct Code8 {
         for (int i = 0; i < N; ++i) r[i / 4] |= code(x[i], inv, word + i * 0x9E3779B1u) << (8 * (i & 3));
     }
 };
-typedef Code8<3, 7, 7> CodeM;     // e4m3
-typedef Code8<2, 14, 15> CodeV;   // e5m2
+typedef Code8<3, 7, 7, 0> CodeM;     // e4m3
+typedef Code8<2, 14, 15, 1> CodeV;   // e5m2
 
 // N codes from any byte on, four to a word.
 typedef uint32_t word_any_t __attribute__((aligned(1)));

@@ -51,6 +51,8 @@ def encode(x, t, kind):
     q = np.floor(np.rint(np.ldexp(a, man - k + bits)) / 2.0 ** bits + u)
     # q steps of 2^(k - man) as a code: q < 2^man only where k = low (the subnormal numbers, exponent field 0)
     code = (k - low) * 2 ** man + q
+    if kind == "V":  # what is not zero is not stored as zero
+        code = np.maximum(code, pad != 0)
     code = np.where(fine, code, 127).astype(np.uint8) | np.where(np.signbit(pad), 128, 0).astype(np.uint8)
     return code.reshape(-1)[:n], scale.astype(f)
 

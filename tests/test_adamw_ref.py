@@ -71,3 +71,48 @@ def test_infinities_and_nan_are_stored_as_nan_and_alone():
     keep[[3, 70]] = False
     assert np.array_equal(code[keep], want[0][keep]) and np.array_equal(scale, want[1])
     assert np.isnan(adamw_ref.decode(code, scale, "M")[[3, 70]]).all()
+
+
+def trajectory(factor, steps, alike, seed=0, blocks=4):
+    """Largest update in units of lr, after a fifth of the steps, of elements that share their block with one whose
+    gradients are `factor` times larger: with 8-bit moments and with fp32 ones.  alike: every step has the same
+    gradients."""
+    rng = np.random.default_rng(seed)
+    n = 128 * blocks
+    size = np.where(np.arange(n) % 128 == 0, 1e-3 * factor, 1e-3)
+    g = rng.normal(size=n) * size
+    M, V = np.zeros(n, np.float32), np.zeros(n, np.float32)
+    codes = [(np.zeros(n, np.uint8), np.ones(blocks, np.float32))] * 2
+    largest = [0.0, 0.0]
+    for t in range(1, steps + 1):
+        if not alike:
+            g = rng.normal(size=n) * size
+        G = g.astype(np.float32)
+        m, v = adamw_ref.moments(G, 1.0, adamw_ref.decode(*codes[0], "M"), adamw_ref.decode(*codes[1], "V"), 0.9, 0.999)
+        codes = [adamw_ref.encode(m, t, "M"), adamw_ref.encode(v, t, "V")]
+        M, V = adamw_ref.moments(G, 1.0, M, V, 0.9, 0.999)
+        if 5 * t > steps:
+            for k, (a, b) in enumerate(((m, v), (M, V))):
+                w, _ = adamw_ref.update(np.zeros(n), a, b, 1.0, 0.9, 0.999, 1e-8, t, 0.0)
+                largest[k] = max(largest[k], np.abs(w)[np.arange(n) % 128 != 0].max())
+    return largest
+
+
+@pytest.mark.parametrize("alike", [False, True])
+@pytest.mark.parametrize("factor", [1.0, 1e4, 3e4, 1e5, 1e6, 1e8])
+def test_no_step_explodes_where_gradients_of_a_block_differ(factor, alike):
+    """|m| / sqrt(v) is at most k = (1 - b1) / sqrt((1 - b2) (1 - b1^2 / b2)) = 7.3 for every sequence of gradients.
+    The cut of M adds at most one of its smallest codes, 2^-16 of the largest M's power of two, where sqrt(v) is
+    at least 2^-15 of the largest V's root: another k / sqrt(2).  Before, V could be zero there: 30000 lr at 3e4."""
+    with_codes, plain = trajectory(factor, 1000, alike)
+    k = 0.1 / np.sqrt(0.001 * (1 - 0.81 / 0.999))
+    assert plain < k and with_codes < k * (1 + 2 ** -0.5)
+
+
+def test_a_second_moment_that_is_not_zero_is_not_stored_as_zero():
+    x = np.zeros(256, np.float32)
+    x[0], x[1], x[2:100], x[130] = 1.0, 1e-45, 1e-20, 1e-45
+    for t in range(1, 50):
+        code, _ = adamw_ref.encode(x, t, "V")
+        assert ((code == 0) == (x == 0)).all()
+        assert (code[1:100] == 1).all()

@@ -293,3 +293,22 @@ def test_tensors_beyond_32_bit_offsets():
     grass.grad_norm(plan, 1.0, out, grass.workspace(grass.grad_norm_workspace(plan)))
     want = math.sqrt(float((last.G.double() ** 2).sum()))
     assert abs(out[0].item() - want) <= 2.0 ** -23 * want
+
+
+@pytest.mark.parametrize("n", [4096, 1000])
+@pytest.mark.parametrize("wdt,gdt", [(F32, F32), (BF16, BF16)])
+def test_blocks_of_gradients_of_very_different_size(wdt, gdt, n):
+    """One element of each 128 with gradients 10^5 times the others': codes as on the CPU over many steps, no V
+    becomes zero, and no step is longer than the 12.5 lr that the moments allow (see test_adamw_ref.py)."""
+    x = Tensor(n, 1, wdt, gdt, True, zero=True)
+    plan = plan_of([x])
+    size = torch.ones(n, device=DEV) * 1e-3
+    size[::128] *= 1e5
+    for t in range(1, 61):
+        x.G.copy_(draw(n, 1000 + t, F32) * size)
+        was = x.w
+        grass.adamw_step(plan, LR, B1, B2, EPS, t)
+        x.check(t)
+        assert int((x.V == 0).sum()) == 0
+        half = torch.finfo(wdt).eps / 2
+        assert (np.abs(x.w - was) <= 12.5 * LR * (1 + FP32) + (half + FP32) * (np.abs(was) + 12.5 * LR)).all()
