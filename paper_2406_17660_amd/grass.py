@@ -672,10 +672,12 @@ _MOMENTS = {torch.float32: (MOMENTS_F32, torch.float32), torch.float8_e4m3fn: (M
 
 class AdamWPlan:
     """Tensors laid out for grass_adamw_step and grass_grad_norm: the plan in device memory, its
-    layout, and the tensors (held, since the plan names their addresses)."""
+    layout, and the tensors (held, since the plan names their addresses; in tuples of its own, so that it
+    does not matter what becomes of the lists they came in)."""
 
     def __init__(self, plan, layout, tensors):
-        self.plan, self.layout, self.tensors = plan, layout, tensors
+        self.plan, self.layout = plan, layout
+        self.tensors = tuple(None if some is None else tuple(some) for some in tensors)
 
 
 def _as_rows(W, G):

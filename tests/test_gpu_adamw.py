@@ -312,3 +312,25 @@ def test_blocks_of_gradients_of_very_different_size(wdt, gdt, n):
         assert int((x.V == 0).sum()) == 0
         half = torch.finfo(wdt).eps / 2
         assert (np.abs(x.w - was) <= 12.5 * LR * (1 + FP32) + (half + FP32) * (np.abs(was) + 12.5 * LR)).all()
+
+
+@pytest.mark.parametrize("q8", [False, True])
+def test_the_callers_lists_may_be_cleared(q8):
+    """The step reaches the tensors that the plan was laid out for, not what is allocated after them."""
+    x = Tensor(4096, 1, F32, F32, q8)
+    e4, e5 = torch.float8_e4m3fn, torch.float8_e5m2
+    lists = [[x.W.clone()], [x.G.clone()], [x.M.clone().view(e4 if q8 else F32)], [x.V.clone().view(e5 if q8 else F32)]]
+    scales = [[x.mscale.clone()], [x.vscale.clone()]] if q8 else [None, None]
+    at = [held[0].data_ptr() for held in lists]
+    plan = grass.adamw_plan(*lists, 0.0, *scales)
+    for held in lists + [s for s in scales if s]:
+        held.clear()
+    others = [torch.full((4096,), 7.0, device=DEV) for _ in range(8)]
+    assert not {o.data_ptr() for o in others} & set(at)
+    grass.adamw_step(plan, LR, B1, B2, EPS, 5)
+    assert all(bool((o == 7.0).all()) for o in others)
+    for mine, held in zip((x.W, x.M, x.V), (plan.tensors[0], plan.tensors[2], plan.tensors[3])):
+        mine.copy_(held[0].view(mine.dtype))
+    if q8:
+        x.mscale, x.vscale = plan.tensors[4][0], plan.tensors[5][0]
+    x.check(5)

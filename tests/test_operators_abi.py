@@ -1,6 +1,8 @@
 """What the norms, AdamW and the gradients' norm refuse on the host, before anything is launched, and how
 a plan is laid out (CPU only)."""
 import ctypes as C
+import gc
+import weakref
 
 import pytest
 import torch
@@ -175,3 +177,18 @@ def test_binding_refuses_host_tensors_and_other_types():
     with pytest.raises(AssertionError):
         grass.adamw_plan([x], [x], [x], [x])
     assert grass.moment_blocks(0) == 0 and grass.moment_blocks(1) == 1 and grass.moment_blocks(129) == 2
+
+
+def test_a_plan_holds_its_tensors_whatever_becomes_of_the_callers_lists():
+    gone = []
+    lists = [[torch.zeros(3)] for _ in range(4)]
+    for held in lists:
+        weakref.finalize(held[0], gone.append, True)
+    plan = grass.AdamWPlan(None, grass.AdamWLayout(), (*lists, None, None))
+    for held in lists:
+        held.clear()
+    gc.collect()
+    assert not gone and [len(held) for held in plan.tensors[:4]] == [1] * 4
+    del plan
+    gc.collect()
+    assert len(gone) == 4
