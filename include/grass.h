@@ -465,7 +465,8 @@ grass_status grass_adam_scatter_replayable(const float* GC, int64_t ldgc, void* 
  * written by RMS).  Sums are fp32 (sums of squares therefore below 2^128); a NaN or an infinity
  * spoils its own row and no other.  H may be X or R, and Y may be X or R (the same address
  * and leading dimension; not H); other overlaps are not allowed.  T = 0 is a no-op; n >= 1.
- * Errors: NULL, SHAPE (also eps negative or NaN), DTYPE. */
+ * Errors: NULL, SHAPE (also eps negative or NaN, and an address that is not a multiple of its type's
+ * size), DTYPE. */
 typedef enum { GRASS_NORM_LAYER = 0, GRASS_NORM_RMS = 1 } grass_norm;
 grass_status grass_norm_forward(grass_norm kind, const void* X, int64_t ldx, const void* R,
                                 int64_t ldr, grass_dtype dt, int64_t T, int64_t n, const void* gain,
@@ -483,7 +484,8 @@ grass_status grass_norm_forward(grass_norm kind, const void* X, int64_t ldx, con
  * fp32, in an order that depends on the sizes alone, so that equal calls give equal bits.  `ws` must
  * hold grass_norm_backward_workspace(...) bytes (NULL where neither dgain nor dbias is wanted).
  * T = 0 writes zeros to dgain and dbias; n >= 1.
- * Errors: NULL, SHAPE, DTYPE, WORKSPACE. */
+ * Errors: NULL, SHAPE (also an address that is not a multiple of its type's size), DTYPE, WORKSPACE
+ * (also `ws` not 4-byte aligned). */
 size_t grass_norm_backward_workspace(int64_t T, int64_t n, grass_dtype dt);
 grass_status grass_norm_backward(grass_norm kind, const void* dY, int64_t lddy, const void* H,
                                  int64_t ldh, const void* dR, int64_t lddr, grass_dtype dt, int64_t T,
@@ -548,7 +550,8 @@ grass_status grass_adamw_plan(int count, const grass_adamw_tensor* tensors, void
  * t (for captured steps; the fourth is t modulo 2^24, which the thresholds are formed from in either
  * case).  grad_scale: NULL (1), or a device float that every gradient is multiplied by, such as
  * the factor of grass_grad_norm; where it is NaN the step changes nothing.
- * Errors: NULL, SHAPE (also t < 1, a beta outside [0,1), a plan of gradients alone), DEVICE. */
+ * Errors: NULL, SHAPE (also t < 1, a beta outside [0,1), a plan of gradients alone, step_scalars or
+ * grad_scale not 4-byte aligned), DEVICE. */
 grass_status grass_adamw_step(const void* plan, const grass_adamw_layout* layout, float lr,
                               float beta1, float beta2, float eps, int64_t t,
                               const float* step_scalars, const float* grad_scale, void* stream);
@@ -560,7 +563,7 @@ grass_status grass_adamw_step_scalars(float lr, float beta1, float beta2, int64_
  * (out: 2 device floats; sums in fp64, in a fixed order).  Where the sum is not finite out[1] is NaN,
  * which makes grass_adamw_step skip the step.  No gradients: 0 and 1.  `ws` must hold
  * grass_grad_norm_workspace(layout) bytes, 8-byte aligned.
- * Errors: NULL, SHAPE (also max_norm negative or NaN), WORKSPACE. */
+ * Errors: NULL, SHAPE (also max_norm negative or NaN, `out` not 4-byte aligned), WORKSPACE. */
 size_t grass_grad_norm_workspace(const grass_adamw_layout* layout);
 grass_status grass_grad_norm(const void* plan, const grass_adamw_layout* layout, float max_norm,
                              float* out, void* ws, size_t ws_bytes, void* stream);

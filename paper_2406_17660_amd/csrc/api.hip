@@ -3,6 +3,7 @@
 // that fails validation has no side effect (and can be exercised on a machine without a
 // GPU).
 #include <atomic>
+#include <initializer_list>
 
 #include "common.hpp"
 
@@ -477,6 +478,13 @@ grass_status grass_gather_rows(const void* G, grass_dtype gdt, int64_t m, int64_
     return launch_gather_rows(G, gdt, n, ldg, idx, rho, r, out, ldo, as_stream(stream));
 }
 
+// Every address (NULL among them) is a multiple of the size of a `dt` value.
+static bool on_elements(grass_dtype dt, std::initializer_list<const void*> addresses) {
+    uintptr_t bits = 0;
+    for (const void* p : addresses) bits |= reinterpret_cast<uintptr_t>(p);
+    return bits % (dt == GRASS_F32 ? 4 : 2) == 0;
+}
+
 static grass_status check_norm(grass_norm kind, grass_dtype dt, grass_dtype gdt, int64_t T, int64_t n) {
     if (T < 0 || n < 1 || !small(T) || !small(n)) return GRASS_ERR_SHAPE;
     if (kind != GRASS_NORM_LAYER && kind != GRASS_NORM_RMS) return GRASS_ERR_DTYPE;
@@ -491,6 +499,9 @@ grass_status grass_norm_forward(grass_norm kind, const void* X, int64_t ldx, con
     if (st != GRASS_OK) return st;
     if (ldx < n || ldy < n || (R && (ldr < n || ldh < n)) || !(eps >= 0.f)) return GRASS_ERR_SHAPE;
     if (!present(X, T) || !present(Y, T) || (R && !present(H, T))) return GRASS_ERR_NULL;
+    if (!on_elements(dt, {X, R, R ? H : nullptr, Y}) || !on_elements(gdt, {gain, bias}) ||
+        !on_elements(GRASS_F32, {kind == GRASS_NORM_LAYER ? mean : nullptr, rstd}))
+        return GRASS_ERR_SHAPE;
     return launch_norm_forward(kind, X, ldx, R, ldr, dt, T, n, gain, bias, gdt, eps, R ? H : nullptr, ldh, Y, ldy,
                                mean, rstd, as_stream(stream));
 }
@@ -511,8 +522,11 @@ grass_status grass_norm_backward(grass_norm kind, const void* dY, int64_t lddy, 
     if (!present(dY, T) || !present(H, T) || !present(rstd, T) || !present(dX, T) ||
         (kind == GRASS_NORM_LAYER && !present(mean, T)))
         return GRASS_ERR_NULL;
+    if (!on_elements(dt, {dY, H, dR, dX}) || !on_elements(gdt, {gain}) ||
+        !on_elements(GRASS_F32, {kind == GRASS_NORM_LAYER ? mean : nullptr, rstd, dgain, dbias}))
+        return GRASS_ERR_SHAPE;
     const size_t need = dgain || dbias ? norm_backward_workspace_bytes(T, n, dt) : 0;
-    if (need > 0 && (!ws || ws_bytes < need)) return GRASS_ERR_WORKSPACE;
+    if (need > 0 && (!ws || ws_bytes < need || !aligned_to(ws, 4))) return GRASS_ERR_WORKSPACE;
     return launch_norm_backward(kind, dY, lddy, H, ldh, dR, lddr, dt, T, n, gain, gdt, mean, rstd, dX, lddx, dgain,
                                 dbias, ws, as_stream(stream));
 }
@@ -584,7 +598,7 @@ grass_status grass_adamw_step(const void* plan, const grass_adamw_layout* layout
     if (st != GRASS_OK) return st;
     if ((!step_scalars && t < 1) || !(beta1 >= 0.f && beta1 < 1.f) || !(beta2 >= 0.f && beta2 < 1.f))
         return GRASS_ERR_SHAPE;
-    if (!adamw_steps(*layout)) return GRASS_ERR_SHAPE;
+    if (!adamw_steps(*layout) || !on_elements(GRASS_F32, {step_scalars, grad_scale})) return GRASS_ERR_SHAPE;
     return launch_adamw(plan, *layout, lr, beta1, beta2, eps, step_scalars ? 1 : t, step_scalars, grad_scale,
                         as_stream(stream));
 }
@@ -608,7 +622,7 @@ grass_status grass_grad_norm(const void* plan, const grass_adamw_layout* layout,
     const grass_status st = check_adamw_plan(plan, layout);
     if (st != GRASS_OK) return st;
     if (!out) return GRASS_ERR_NULL;
-    if (!(max_norm >= 0.f)) return GRASS_ERR_SHAPE;
+    if (!(max_norm >= 0.f) || !on_elements(GRASS_F32, {out})) return GRASS_ERR_SHAPE;
     const size_t need = grad_norm_workspace_bytes(*layout);
     if (need > 0 && (!ws || ws_bytes < need || !aligned_to(ws, 8))) return GRASS_ERR_WORKSPACE;
     return launch_grad_norm(plan, *layout, max_norm, out, ws, as_stream(stream));

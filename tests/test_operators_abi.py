@@ -192,3 +192,25 @@ def test_a_plan_holds_its_tensors_whatever_becomes_of_the_callers_lists():
     del plan
     gc.collect()
     assert len(gone) == 4
+
+
+@pytest.mark.parametrize("kw", [
+    dict(X=ODD), dict(R=ODD), dict(H=ODD), dict(Y=ODD), dict(dt=0, X=FAKE + 2), dict(dt=0, R=FAKE + 2), dict(dt=0, H=FAKE + 2),
+    dict(dt=0, Y=FAKE + 2), dict(gain=FAKE + 2), dict(bias=FAKE + 2), dict(gdt=1, gain=ODD), dict(gdt=1, bias=ODD),
+    dict(mean=FAKE + 2), dict(rstd=ODD)])
+def test_norm_forward_refuses_addresses_between_elements(kw):
+    assert forward(**kw) == SHAPE
+
+
+@pytest.mark.parametrize("want,kw", [
+    (SHAPE, dict(dY=ODD)), (SHAPE, dict(H=ODD)), (SHAPE, dict(dR=ODD)), (SHAPE, dict(dX=ODD)), (SHAPE, dict(dt=0, dY=FAKE + 2)),
+    (SHAPE, dict(dt=0, H=FAKE + 2)), (SHAPE, dict(dt=0, dR=FAKE + 2)), (SHAPE, dict(dt=0, dX=FAKE + 2)), (SHAPE, dict(gain=FAKE + 2)),
+    (SHAPE, dict(gdt=1, gain=ODD)), (SHAPE, dict(mean=FAKE + 2)), (SHAPE, dict(rstd=ODD)), (SHAPE, dict(dgain=FAKE + 2)),
+    (SHAPE, dict(dbias=FAKE + 2)), (WS, dict(ws=FAKE + 2)), (WS, dict(ws=ODD))])
+def test_norm_backward_refuses_addresses_between_elements(want, kw):
+    assert backward(**kw) == want
+
+
+def test_adamw_and_grad_norm_refuse_addresses_between_elements():
+    assert step(scalars=FAKE + 2) == step(scale=ODD) == SHAPE
+    assert norm(out=FAKE + 2) == norm(out=ODD) == SHAPE
