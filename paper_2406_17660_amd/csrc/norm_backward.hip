@@ -342,16 +342,17 @@ __global__ __launch_bounds__(kWide) void backward_wide_kernel(BackwardArgs a) {
     }
 }
 
-// dgain and dbias from the P blocks' sums.  A block: 64 columns; its sixteen wavefronts take every
-// sixteenth row each.  P = 0 writes zeros.
+// dgain and dbias from the P blocks' sums.  A block: 64 columns, of those from `first` on; its sixteen wavefronts
+// take every sixteenth row each.  P = 0 writes zeros.
 constexpr int kSumWaves = 16;
+constexpr int64_t kMostColumns = int64_t{1} << 27;  // of one launch
 __global__ __launch_bounds__(kSumWaves* kWave) void column_sums_kernel(const float* __restrict__ part, int P, int n,
-                                                                       float* dgain, float* dbias) {
+                                                                       int first, float* dgain, float* dbias) {
     __shared__ float sums[kSumWaves][kWave];
     float* out = blockIdx.y ? dbias : dgain;
     if (!out) return;
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    const int64_t c = static_cast<int64_t>(blockIdx.x) * kWave + lane;
+    const int64_t c = first + static_cast<int64_t>(blockIdx.x) * kWave + lane;
     float s = 0.f;
     if (c < n) {
         const float* p = part + static_cast<int64_t>(blockIdx.y) * n + c;
@@ -453,10 +454,12 @@ grass_status launch_norm_backward(grass_norm kind, const void* dY, int64_t lddy,
                              sums ? static_cast<float*>(ws) : nullptr, 0, dgain, dbias};
         done = (dt == GRASS_F32 ? launch<float>(a, s) : launch<uint16_t>(a, s)) || done;
     }
-    if (!done) {
-        const dim3 grid(static_cast<unsigned>((n + kWave - 1) / kWave), 2);
+    // (a grid has fewer than 2^32 threads: 16 of them for each column here)
+    for (int64_t first = 0; !done && first < n; first += kMostColumns) {
+        const int64_t columns = n - first < kMostColumns ? n - first : kMostColumns;
+        const dim3 grid(static_cast<unsigned>((columns + kWave - 1) / kWave), 2);
         column_sums_kernel<<<grid, kSumWaves * kWave, 0, s>>>(static_cast<const float*>(ws), backward_blocks(T, n, dt),
-                                                              static_cast<int>(n), dgain, dbias);
+                                                              static_cast<int>(n), static_cast<int>(first), dgain, dbias);
     }
     return launch_status();
 }

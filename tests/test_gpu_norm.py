@@ -346,3 +346,20 @@ def test_rows_beyond_32_bit_offsets():
     check_forward(X.contiguous(), None, None, None, "layer", Y.contiguous(), None, mean, rstd)
     dX, dgain, dbias = gpu_backward(dY, X, None, mean, rstd, "layer", dX=Y)
     check_backward(dY.contiguous(), X.contiguous(), None, mean, rstd, "layer", None, dX.contiguous(), dgain, dbias)
+
+
+@pytest.mark.parametrize("T", [0, 1])
+def test_more_columns_than_a_grid_of_their_sums_has_threads_for(T):
+    """16 threads for each column's sum: 2^28 columns are 2^32 threads.  One row: its sums are single products."""
+    n = (1 << 28) + 100
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(11)
+    dY, H = (torch.empty((T, n), dtype=torch.bfloat16, device=DEV).normal_(generator=gen) for _ in range(2))
+    rstd = torch.full((T,), 0.5, device=DEV)
+    dX, dgain, dbias = gpu_backward(dY, H, None, None, rstd, "rms")
+    if T == 0:
+        assert int(torch.count_nonzero(dgain)) == 0 and int(torch.count_nonzero(dbias)) == 0
+        return
+    assert torch.equal(dbias, dY[0].float())
+    assert torch.equal(dgain, dY[0].float() * (H[0].float() * 0.5))
+    assert torch.isfinite(dX).all()
