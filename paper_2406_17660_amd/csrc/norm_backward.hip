@@ -343,8 +343,9 @@ __global__ __launch_bounds__(kWide) void backward_wide_kernel(BackwardArgs a) {
 }
 
 // dgain and dbias from the P blocks' sums.  A block: 64 columns, of those from `first` on; its sixteen wavefronts
-// take every sixteenth row each.  P = 0 writes zeros.
-constexpr int kSumWaves = 16;
+// take every sixteenth row each, all of them under way at once, however many there are (a loop over P asked for
+// them one by one where P was not 256: 2000 x 500 bf16 10.8 us with both kernels, so 7.3).  P = 0 writes zeros.
+constexpr int kSumWaves = 16, kSumRows = kUnits / kSumWaves;
 constexpr int64_t kMostColumns = int64_t{1} << 27;  // of one launch
 __global__ __launch_bounds__(kSumWaves* kWave) void column_sums_kernel(const float* __restrict__ part, int P, int n,
                                                                        int first, float* dgain, float* dbias) {
@@ -356,8 +357,14 @@ __global__ __launch_bounds__(kSumWaves* kWave) void column_sums_kernel(const flo
     float s = 0.f;
     if (c < n) {
         const float* p = part + static_cast<int64_t>(blockIdx.y) * n + c;
-#pragma unroll 16
-        for (int k = wave; k < P; k += kSumWaves) s += p[static_cast<int64_t>(k) * 2 * n];
+        float x[kSumRows];
+#pragma unroll
+        for (int j = 0; j < kSumRows; ++j) {
+            const int k = wave + j * kSumWaves;
+            x[j] = k < P ? p[static_cast<int64_t>(k) * 2 * n] : 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < kSumRows; ++j) s += x[j];
     }
     sums[wave][lane] = s;
     __syncthreads();

@@ -363,3 +363,12 @@ def test_more_columns_than_a_grid_of_their_sums_has_threads_for(T):
     assert torch.equal(dbias, dY[0].float())
     assert torch.equal(dgain, dY[0].float() * (H[0].float() * 0.5))
     assert torch.isfinite(dX).all()
+
+
+@pytest.mark.parametrize("T,n,dtype", [(769, 64, torch.bfloat16), (1999, 250, torch.bfloat16), (2000, 500, torch.bfloat16),
+                                       (1017, 1032, torch.float32), (800, 2056, torch.bfloat16), (1020, 1536, torch.float32)])
+def test_sums_of_fewer_than_256_workgroups(T, n, dtype):
+    """25 to 250 rows of partial sums, which no multiple of 16 divides."""
+    dY, H, gain = draw((T, n), 5, dtype, 0.3, 0.05), draw((T, n), 6, dtype, 1.5, 0.4), draw(n, 1, torch.float32, 0.2, 1.0)
+    mean, rstd = stats(H, "layer")
+    check_backward(dY, H, gain, mean, rstd, "layer", None, *gpu_backward(dY, H, gain, mean, rstd, "layer"))
