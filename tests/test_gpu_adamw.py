@@ -334,3 +334,16 @@ def test_the_callers_lists_may_be_cleared(q8):
     if q8:
         x.mscale, x.vscale = plan.tensors[4][0], plan.tensors[5][0]
     x.check(5)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_grad_norm_of_more_than_the_cache_holds(dtype):
+    """Beyond 128 MB the reads carry the streaming hint, where both chunks of a turn start on 16 bytes."""
+    n = 160 * (1 << 20) // dtype.itemsize
+    whole = draw(n + 6 * 3000, 1, dtype, 0.01)
+    Gs = [whole[:n]] + [whole[n + 3000 * i + i:n + 3000 * (i + 1)] for i in range(6)]
+    want = math.sqrt(sum(float((g.double() ** 2).sum()) for g in Gs))
+    norm, factor = gpu_grad_norm(Gs, 0.5)
+    assert abs(norm - want) <= 2.0 ** -23 * want
+    assert abs(factor - 0.5 / want) <= 2.0 ** -23 * 0.5 / want
+    assert (norm, factor) == tuple(gpu_grad_norm(Gs, 0.5))

@@ -6,6 +6,9 @@ wide rows used here) and then a tree, so that its error is below 100 half steps 
 the magnitudes; the other operations add a few.  FP32 = 128 * 2^-24 of the magnitudes that
 enter an output covers both.  Sums over tokens run through at most T terms, or 300 + T / 256 where
 many rows are summed by several workgroups."""
+import os
+import re
+
 import numpy as np
 import pytest
 import torch
@@ -372,3 +375,114 @@ def test_sums_of_fewer_than_256_workgroups(T, n, dtype):
     dY, H, gain = draw((T, n), 5, dtype, 0.3, 0.05), draw((T, n), 6, dtype, 1.5, 0.4), draw(n, 1, torch.float32, 0.2, 1.0)
     mean, rstd = stats(H, "layer")
     check_backward(dY, H, gain, mean, rstd, "layer", None, *gpu_backward(dY, H, gain, mean, rstd, "layer"))
+
+
+@pytest.mark.parametrize("T,n,dtype", [(1024, 64, torch.bfloat16), (4099, 128, torch.float32), (4100, 512, torch.bfloat16),
+                                       (3001, 1000, torch.bfloat16), (2600, 2056, torch.float32), (1500, 4096, torch.bfloat16),
+                                       (1100, 5461, torch.bfloat16), (1030, 16385, torch.bfloat16), (2000, 1293, torch.float32),
+                                       (1500, 2055, torch.bfloat16), (900, 4097, torch.bfloat16), (1200, 8193, torch.bfloat16),
+                                       (500, 9001, torch.float32), (800, 16383, torch.float32)])
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+def test_more_rows_than_workgroups_with_a_residual_branch(T, n, dtype, kind):
+    """R and dR of the second row of a turn and after, and of the two kernels' path, against 64 bits."""
+    gain, bias = draw(n, 1, torch.float32, 0.2, 1.0), draw(n, 2, torch.float32, 0.2)
+    X, R = draw((T, n), 3, dtype, 1.5, 0.4), draw((T, n), 4, dtype)
+    Y, H, mean, rstd = nan((T, n), dtype), nan((T, n), dtype), nan((T,)), nan((T,))
+    grass.norm_forward(X, gain, bias, EPS, Y, KINDS[kind], R=R, H=H, mean=mean, rstd=rstd)
+    check_forward(X, R, gain, bias, kind, Y, H, mean if kind == "layer" else None, rstd)
+    dY, dR = draw((T, n), 5, dtype, 0.3, 0.05), draw((T, n), 7, dtype, 0.3)
+    got = gpu_backward(dY, H, gain, mean, rstd, kind, dR)
+    check_backward(dY, H, gain, mean if kind == "layer" else None, rstd, kind, dR, *got)
+
+
+def streamed_bytes():
+    """From so many bytes on accesses carry the streaming hint and the forward pass has more workgroups."""
+    with open(os.path.join(os.path.dirname(__file__), "..", "paper_2406_17660_amd", "csrc", "elem.hpp")) as f:
+        return float(re.search(r"kStreamed = ([0-9.]+) \* \(1 << 20\);", f.read()).group(1)) * (1 << 20)
+
+
+STREAMED = [(64, torch.float32, 0, 3), (100, torch.bfloat16, 0, 3), (128, torch.bfloat16, 0, 3), (250, torch.bfloat16, 0, 1),
+            (256, torch.bfloat16, 0, 3), (500, torch.bfloat16, 0, 1), (512, torch.bfloat16, 0, 2), (512, torch.float32, 8, 1),
+            (601, torch.float32, 0, 1), (1000, torch.bfloat16, 0, 1), (1293, torch.bfloat16, 3, 1), (1536, torch.bfloat16, 0, 1),
+            (2056, torch.bfloat16, 0, 1), (2601, torch.float32, 0, 1), (4096, torch.bfloat16, 0, 3), (4096, torch.float32, 0, 1),
+            (4200, torch.bfloat16, 0, 1), (5461, torch.bfloat16, 0, 1), (5461, torch.float32, 1, 1), (8200, torch.bfloat16, 0, 1),
+            (12289, torch.float32, 0, 1), (16384, torch.bfloat16, 0, 1), (16384, torch.float32, 0, 1)]
+
+
+def streamed_rows(n, dtype, arrays, times):
+    """Rows just beyond the limit, so many times over, whose last turn is partly filled."""
+    size = n * dtype.itemsize * arrays
+    T = int(times * streamed_bytes() // size) + 37
+    assert T * size > streamed_bytes()
+    return T
+
+
+def rows_of(T, n, seed, dtype, more, scale=1.0, shift=0.0):
+    values = draw((T, n), seed, dtype, scale, shift)
+    return padded(values, n + more, 1)[0] if more else values
+
+
+@pytest.mark.parametrize("n,dtype,more,times", STREAMED)
+@pytest.mark.parametrize("add", [False, True])
+def test_forward_of_more_than_the_cache_holds(n, dtype, more, times, add):
+    """Against the formulas in 64 bits, with the bounds of check_forward."""
+    T, layer = streamed_rows(n, dtype, 4 if add else 2, times), n % 3 != 0
+    gain, bias = draw(n, 1, torch.float32, 0.2, 1.0), draw(n, 2, torch.float32, 0.2)
+    X, R = rows_of(T, n, 3, dtype, more, 1.5, 0.4), rows_of(T, n, 4, dtype, more) if add else None
+    Y, H = nan((T, n + more), dtype)[:, :n], nan((T, n + more), dtype)[:, :n] if add else None
+    mean, rstd = nan((T,)), nan((T,))
+    grass.norm_forward(X, gain, bias, EPS, Y, grass.NORM_LAYER if layer else grass.NORM_RMS, R=R, H=H, mean=mean, rstd=rstd)
+    for a in range(0, T, max(1, (1 << 24) // n)):
+        at = slice(a, a + max(1, (1 << 24) // n))
+        h = X[at]
+        if add:
+            h = (h.float() + R[at].float()).to(dtype)
+            assert torch.equal(H[at], h)
+        h = h.double()
+        size = h.abs().mean(1, keepdim=True)
+        mu = h.mean(1, keepdim=True) if layer else torch.zeros_like(size)
+        d = h - mu
+        rs = 1.0 / torch.sqrt((d * d).mean(1, keepdim=True) + EPS)
+        y = d * rs * gain.double() + bias.double()
+        assert ((Y[at].double() - y).abs() <= half(dtype) * y.abs() * (1 + FP32) +
+                FP32 * (size * rs * gain.double().abs() + y.abs() + bias.double().abs())).all()
+        if layer:
+            assert ((mean[at].double() - mu[:, 0]).abs() <= FP32 * size[:, 0]).all()
+        assert ((rstd[at].double() - rs[:, 0]).abs() <= (FP32 + (FP32 * size * rs)[:, 0] ** 2) * rs[:, 0]).all()
+    if more:
+        assert int((~torch.isnan(Y.as_strided((T - 1, more), (n + more, 1), n).float())).sum()) == 0
+
+
+@pytest.mark.parametrize("n,dtype,more,times", STREAMED)
+@pytest.mark.parametrize("add", [False, True])
+def test_backward_of_more_than_the_cache_holds(n, dtype, more, times, add):
+    """Against the formulas in 64 bits, with the bounds of check_backward."""
+    T, layer = streamed_rows(n, dtype, 4 if add else 3, 1), n % 3 != 0
+    gain = draw(n, 1, torch.float32, 0.2, 1.0)
+    dY, H = rows_of(T, n, 5, dtype, more, 0.3, 0.05), rows_of(T, n, 6, dtype, more, 1.5, 0.4)
+    dR = rows_of(T, n, 7, dtype, more, 0.3) if add else None
+    mean = H.double().mean(1).float() if layer else None
+    h = H.double() - mean.double()[:, None] if layer else H.double()
+    rstd = (1.0 / torch.sqrt((h * h).mean(1) + EPS)).float()
+    dX = nan((T, n + more), dtype)[:, :n]
+    _, dgain, dbias = gpu_backward(dY, H, gain, mean, rstd, "layer" if layer else "rms", dR, dX)
+    sums = torch.zeros((4, n), dtype=torch.float64, device=DEV)
+    for a in range(0, T, max(1, (1 << 24) // n)):
+        at = slice(a, a + max(1, (1 << 24) // n))
+        dy, rs = dY[at].double(), rstd[at].double()[:, None]
+        xh = h[at] * rs
+        z = dy * gain.double()
+        dx = z - xh * (z * xh).mean(1, keepdim=True)
+        if layer:
+            dx = dx - z.mean(1, keepdim=True)
+        dx = dx * rs
+        size = rs * (z.abs() + z.abs().mean(1, keepdim=True) + xh.abs() * (z * xh).abs().mean(1, keepdim=True))
+        if add:
+            dx, size = dx + dR[at].double(), size + dR[at].double().abs()
+        assert ((dX[at].double() - dx).abs() <= half(dtype) * dx.abs() * (1 + FP32) + FP32 * size).all()
+        for k, term in enumerate((dy * xh, dy, (dy * xh).abs(), dy.abs())):
+            sums[k] += term.sum(0)
+    for got, want, size in ((dgain, sums[0], sums[2]), (dbias, sums[1], sums[3])):
+        assert ((got.double() - want).abs() <= depth(T) * 2.0 ** -24 * size).all()
+    if more:
+        assert int((~torch.isnan(dX.as_strided((T - 1, more), (n + more, 1), n).float())).sum()) == 0
