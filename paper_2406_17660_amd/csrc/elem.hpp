@@ -207,19 +207,19 @@ struct RowShape {
 constexpr int kWidestRow = 16384;  // values of a row that stay in registers
 // The shape for a row of n values, as a call of f with it.  Two vectors per thread, so that a workgroup
 // has 16 KB of each array under way, or three where two of twice as many threads would leave a quarter of them and
-// more without work; more for the widest rows, one for the narrowest.
-template <typename T, typename F>
-void by_shape(int64_t n, F&& f) {
+// more without work and three(threads of such a row) says so; more for the widest rows, one for the narrowest.
+template <typename T, typename Three, typename F>
+void by_shape(int64_t n, Three&& three, F&& f) {
     const int64_t vectors = (n * static_cast<int64_t>(sizeof(T)) + 15) / 16;
     if (vectors <= 16) f(RowShape<16, 1, 0>{});
     else if (vectors <= 32) f(RowShape<32, 1, 0>{});
     else if (vectors <= 64) f(RowShape<64, 1, 0>{});
     else if (vectors <= 128) f(RowShape<64, 2, 1>{});
-    else if (vectors <= 192) f(RowShape<64, 3, 2>{});
+    else if (vectors <= 192 && three(64)) f(RowShape<64, 3, 2>{});
     else if (vectors <= 256) f(RowShape<128, 2, 1>{});
-    else if (vectors <= 384) f(RowShape<128, 3, 2>{});
+    else if (vectors <= 384 && three(128)) f(RowShape<128, 3, 2>{});
     else if (vectors <= 512) f(RowShape<256, 2, 1>{});
-    else if (vectors <= 768) f(RowShape<256, 3, 2>{});
+    else if (vectors <= 768 && three(256)) f(RowShape<256, 3, 2>{});
     else if (vectors <= 1024) f(RowShape<512, 2, 1>{});
     else if (vectors <= 1536) f(RowShape<512, 3, 2>{});
     else if (vectors <= 2048) f(RowShape<512, 4, 3>{});

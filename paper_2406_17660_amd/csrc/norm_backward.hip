@@ -375,46 +375,63 @@ __global__ __launch_bounds__(kSumWaves* kWave) void column_sums_kernel(const flo
     out[c] = s;
 }
 
+// Three vectors a thread (which hold sums and gain of their own: 228 registers where two take 153), two / three us.  Rows of 64
+// lanes: bf16 161342 x 1033 253 / 210, 34090 x 1100 with dR 57 / 61, 18151 x 1033 with dR 42 / 38, fp32 109649 x 760 170 / 194: bf16 without
+// dR or on odd 2-byte boundaries.  Of 128: bf16 81024 x 2057 262 / 211, 1537 x 2601 13.7 / 13.9, fp32 80671 x 1033 199 / 180: all.  Of 256:
+// bf16 30519 x 5461 226 / 191, 1525 x 5461 18.2 / 19.7, in windows 11904 x 4200 59.9 / 60.9, fp32 37810 x 2204 195 / 177, 1890 x 2204
+// 13.9 / 14.9: where the call streams and its rows are fp32 or start anywhere.
 template <typename T>
-int64_t row_groups(int64_t n) {
-    int64_t rows = 1;
-    if (in_registers<T>(n)) by_shape<T>(n, [&](auto shape) { rows = decltype(shape)::B / decltype(shape)::TPR; });
-    return rows;
+bool three_vectors(int tpr, bool streamed, bool window, bool on_words, bool add) {
+    if (tpr == 64) return sizeof(T) == 2 && (!add || !on_words);
+    return tpr == 128 || (streamed && (sizeof(T) == 4 || !window));
 }
 
-// Blocks, each of which leaves one row of column sums: one per compute unit.  2047 x 5461 bf16: 256 of them 19 us, 192
-// 23, 128 30; 512 leave twice the sums: 30 with both kernels against 23.
-int backward_blocks(int64_t T, int64_t n, grass_dtype dt) {
-    const int64_t rows = dt == GRASS_F32 ? row_groups<float>(n) : row_groups<uint16_t>(n);
-    const int64_t want = (T + rows - 1) / rows;
+// Blocks, each of which leaves one row of column sums: one per compute unit.
+int blocks_of(int64_t T, int64_t rows_each) {
+    const int64_t want = (T + rows_each - 1) / rows_each;
     return static_cast<int>(want < kUnits ? want : kUnits);
 }
 
-// Rows up to which dgain and dbias are added up beside dX in one launch.  180 rows, one launch and two: 4096
-// bf16 8.3 and 10.8 us, 7162 fp32 8.5 and 16.4; 546 rows: 9.3 and 12.6, 17.7 and 22.7, 233 bf16 9.4 and 10.8;
-// 1000 rows: 13.9 and 14.1, 28.3 and 29.8, 14.1 and 10.8.
+// The most blocks that a call may take: of the shape with the fewest rows to a block.
+template <typename T>
+int most_blocks(int64_t rows, int64_t n) {
+    int64_t rows_each = 1;
+    if (in_registers<T>(n))
+        by_shape<T>(n, [](int) { return false; }, [&](auto shape) { rows_each = decltype(shape)::B / decltype(shape)::TPR; });
+    return blocks_of(rows, rows_each);
+}
+
+// Rows up to which dgain and dbias are added up beside dX in one launch.  180 rows, one launch and two, in a graph: 4096
+// bf16 5.0 and 9.0 us, 7162 fp32 7.0 and 11.5, 250 bf16 4.5 and 5.8; 546 rows: 9.6 and 12.3, 14.6 and 17.8, 6.5 and 5.9;
+// 1000 rows: 13.9 and 13.0, 26.5 and 25.4, 8.5 and 6.1.  (Outside a graph the second launch costs the host another 3 us.)
 constexpr int64_t kFewRows = 768;
 
-// True where dgain and dbias are done with, false where the blocks' sums wait to be added.
+// The number of blocks whose sums wait to be added; 0 where dgain and dbias are done with (or not wanted).
 template <typename T>
-bool launch(BackwardArgs a, hipStream_t s) {
-    const unsigned rows = static_cast<unsigned>(backward_blocks(a.T, a.n, sizeof(T) == 4 ? GRASS_F32 : GRASS_BF16));
+int launch(BackwardArgs a, hipStream_t s) {
     if (!in_registers<T>(a.n)) {
+        const int blocks = a.part ? blocks_of(a.T, 1) : 0;
         if (a.part) {
-            const dim3 g(static_cast<unsigned>((a.n + int64_t{kWide} * 8 - 1) / (kWide * 8)), rows);
+            const dim3 g(static_cast<unsigned>((a.n + int64_t{kWide} * 8 - 1) / (kWide * 8)), static_cast<unsigned>(blocks));
             backward_wide_sums_kernel<T><<<g, kWide, 0, s>>>(a);
         }
         backward_wide_kernel<T><<<static_cast<unsigned>(a.T < kMostBlocks ? a.T : kMostBlocks), kWide, 0, s>>>(a);
-        return false;
+        return blocks;
     }
-    const auto on16 = [](const void* p, int64_t ld) { return aligned_to(p, 16) && ld * sizeof(T) % 16 == 0; };
-    const bool window = a.n * sizeof(T) % 16 == 0 && on16(a.dY, a.lddy) && on16(a.H, a.ldh) && on16(a.dX, a.lddx) &&
-                        (!a.dR || on16(a.dR, a.lddr));
+    const auto all_on = [&](size_t bytes) {  // every row starts on so many bytes
+        const auto on = [&](const void* p, int64_t ld) { return aligned_to(p, bytes) && ld * sizeof(T) % bytes == 0; };
+        return on(a.dY, a.lddy) && on(a.H, a.ldh) && on(a.dX, a.lddx) && (!a.dR || on(a.dR, a.lddr));
+    };
+    const bool window = a.n * sizeof(T) % 16 == 0 && all_on(16);
     const bool once = static_cast<double>(a.T) * a.n * sizeof(T) * (a.dR ? 4 : 3) > kStreamed;
-    const auto run = [&](unsigned column_blocks, unsigned row_blocks) {
+    const auto three = [&](int tpr) { return three_vectors<T>(tpr, once, window, all_on(4), a.dR != nullptr); };
+    const auto run = [&](unsigned column_blocks, bool rows_too) {
         a.column_blocks = column_blocks;
-        by_shape<T>(a.n, [&](auto shape) {
+        int blocks = 0;
+        by_shape<T>(a.n, three, [&](auto shape) {
             typedef decltype(shape) S;
+            blocks = rows_too ? blocks_of(a.T, S::B / S::TPR) : 0;
+            const unsigned row_blocks = static_cast<unsigned>(blocks);
             const auto go = [&](auto win, auto add, auto stream) {
                 backward_kernel<T, S, decltype(win)::value, decltype(add)::value, decltype(stream)::value>
                     <<<column_blocks + row_blocks, S::B, 0, s>>>(a);
@@ -425,27 +442,28 @@ bool launch(BackwardArgs a, hipStream_t s) {
                 if (window) return with_window(std::true_type{});
             with_window(std::false_type{});
         });
+        return blocks;
     };
     if (!a.part || a.T > kFewRows) {
-        run(0, rows);
-        return false;
+        const int blocks = run(0, true);
+        return a.part ? blocks : 0;
     }
     a.part = nullptr;
     constexpr int kColumns = kColumnLanes * 16 / static_cast<int>(sizeof(T));
     const unsigned columns = static_cast<unsigned>((a.n + kColumns - 1) / kColumns);
     if (a.dX != a.dY && a.dX != a.H) {
-        run(columns, rows);
+        run(columns, true);
     } else {  // dX overwrites what the columns' sums read
-        run(columns, 0);
-        run(0, rows);
+        run(columns, false);
+        run(0, true);
     }
-    return true;
+    return 0;
 }
 
 }  // namespace
 
 size_t norm_backward_workspace_bytes(int64_t T, int64_t n, grass_dtype dt) {
-    return static_cast<size_t>(backward_blocks(T, n, dt)) * 2 * n * sizeof(float);
+    return static_cast<size_t>(dt == GRASS_F32 ? most_blocks<float>(T, n) : most_blocks<uint16_t>(T, n)) * 2 * n * sizeof(float);
 }
 
 grass_status launch_norm_backward(grass_norm kind, const void* dY, int64_t lddy, const void* H, int64_t ldh,
@@ -454,18 +472,19 @@ grass_status launch_norm_backward(grass_norm kind, const void* dY, int64_t lddy,
                                   void* dX, int64_t lddx, float* dgain, float* dbias, void* ws, hipStream_t s) {
     const bool sums = dgain || dbias;
     if (T == 0 && !sums) return GRASS_OK;
-    bool done = !sums;
+    int blocks = 0;  // without tokens dgain and dbias are sums of nothing
     if (T > 0) {
         const BackwardArgs a{dY, H, dR, gain, dX, lddy, ldh, lddr, lddx, T, static_cast<int>(n),
                              kind == GRASS_NORM_LAYER, gdt == GRASS_BF16, dbias != nullptr, mean, rstd,
                              sums ? static_cast<float*>(ws) : nullptr, 0, dgain, dbias};
-        done = (dt == GRASS_F32 ? launch<float>(a, s) : launch<uint16_t>(a, s)) || done;
+        blocks = dt == GRASS_F32 ? launch<float>(a, s) : launch<uint16_t>(a, s);
+        if (blocks == 0) return launch_status();
     }
     // (a grid has fewer than 2^32 threads: 16 of them for each column here)
-    for (int64_t first = 0; !done && first < n; first += kMostColumns) {
+    for (int64_t first = 0; first < n; first += kMostColumns) {
         const int64_t columns = n - first < kMostColumns ? n - first : kMostColumns;
         const dim3 grid(static_cast<unsigned>((columns + kWave - 1) / kWave), 2);
-        column_sums_kernel<<<grid, kSumWaves * kWave, 0, s>>>(static_cast<const float*>(ws), backward_blocks(T, n, dt),
+        column_sums_kernel<<<grid, kSumWaves * kWave, 0, s>>>(static_cast<const float*>(ws), blocks,
                                                               static_cast<int>(n), static_cast<int>(first), dgain, dbias);
     }
     return launch_status();

@@ -270,7 +270,12 @@ void launch(const ForwardArgs& a, hipStream_t s) {
     const bool window = a.n * sizeof(T) % 16 == 0 && on16(a.X, a.ldx) && on16(a.Y, a.ldy) &&
                         (!a.R || (on16(a.R, a.ldr) && on16(a.H, a.ldh)));
     const bool once = static_cast<double>(a.T) * a.n * sizeof(T) * (a.R ? 4 : 2) > kStreamed;
-    by_shape<T>(a.n, [&](auto shape) {
+    // Three vectors a thread put more rows into a workgroup.  With R, two / three us: rows of 64 lanes 2320 x 1293 bf16 8.8 / 9.9,
+    // 6050 x 1033 14.5 / 12.5, so from two workgroups per compute unit on; wider ones 3038 x 2057 14.5 / 15.0, 1249 x 5001 12.7 / 13.6,
+    // 60768 x 2057 242 / 222, 24995 x 5001 233 / 199, so where the call streams.  Without R at any number of rows: 5808 x 1033 9.6 / 8.1,
+    // 242013 x 1033 258 / 204, 12019 x 520 fp32 11.6 / 8.6; rows of 128 and 256 lanes win and lose a tenth by how many turns are left.
+    const auto three = [&](int tpr) { return !a.R || (tpr == 64 ? a.T >= 2 * kUnits * (512 / tpr) : once); };
+    by_shape<T>(a.n, three, [&](auto shape) {
         typedef decltype(shape) S;
         constexpr int64_t kRows = S::B / S::TPR;
         const bool two_turns = sizeof(T) == 4 || (a.R && (window || S::TPR < kWave));
