@@ -249,15 +249,27 @@ __global__ __launch_bounds__(kWide) void forward_wide_kernel(ForwardArgs a) {
 }
 
 // Blocks for so many groups of rows.  Short of kStreamed bytes two per compute unit, which walk the rest; from there
-// on whole multiples of that, for 16 turns or more (a few blocks beyond it would be a round of their own), or, where
-// what a block starts with (gain, bias, the first row's way) is small against a turn, one for two turns.  TB/s, means over
-// twenty widths from 200 to 16000 (240 MB to 2 GB), two per unit / 16 turns / 2 turns: bf16 without R 5.07 / 5.06 / 4.51, with R 5.13 /
-// 5.08 / 5.26, fp32 5.38 / 5.31 / 5.47; this rule 5.14, 5.33 and 5.46.
-int64_t forward_blocks(int64_t groups, bool once, bool two_turns) {
+// on as many as take so many turns, 16 in whole multiples of that (a few blocks beyond them would be a round of their own).
+int64_t forward_blocks(int64_t groups, bool once, int turns) {
     const int64_t some = 2 * kUnits;
     if (groups < some || !once) return groups < some ? groups : some;
-    const int64_t more = two_turns ? groups / 2 : groups / (16 * some) * some;
+    const int64_t more = turns < 16 ? groups / turns : groups / (16 * some) * some;
     return more > some ? more : some;
+}
+
+// Turns of a block where the call streams: few where what it starts with (gain, bias, the first row's way) is small against a
+// turn.  TB/s at 1.2 GB with 2, 4 and 16 turns.  fp32: 512 values 5.98 5.94 5.59, 4096 6.18 6.05 6.01, 3001 5.42 5.41 5.13,
+// with R 512 5.96 5.74 5.56.  bf16 with R: 512 5.98 5.68 5.30, 4096 6.02 5.76 5.88, 200 5.51 5.29 4.65, 500 (no window) 5.22 4.91 4.37,
+// 2601 (no window) 3.99 4.33 4.97.  bf16 without: 512 5.83 6.11 5.38, 2048 6.11 6.08 5.83, 200 4.98 5.33 4.97, 501 5.02 5.16 4.54,
+// 2601 3.74 4.09 4.76, 2200 (three vectors) 4.17 4.69 5.27; 64, which half of a row's lanes have no part of, 3.48 3.90 4.23 (80, with
+// five eighths at work, 4.21 4.44 3.99 at 180 MB and 4.16 4.75 4.94).
+template <typename T, typename S>
+int forward_turns(int64_t n, bool add, bool window) {
+    if (sizeof(T) == 4) return 2;
+    const bool two = S::V <= 2;
+    if (add) return window || (two && S::TPR <= kWave) ? 2 : 16;
+    if (two && window && S::TPR >= kWave && S::TPR <= 2 * kWave) return 2;  // (shorter rows take no windows)
+    return two && S::TPR <= kWave && n * sizeof(T) * 8 >= S::TPR * S::V * 16 * 5 ? 4 : 16;
 }
 
 template <typename T>
@@ -278,9 +290,8 @@ void launch(const ForwardArgs& a, hipStream_t s) {
     by_shape<T>(a.n, three, [&](auto shape) {
         typedef decltype(shape) S;
         constexpr int64_t kRows = S::B / S::TPR;
-        const bool two_turns = sizeof(T) == 4 || (a.R && (window || S::TPR < kWave));
         // (a grid has fewer than 2^32 threads)
-        const int64_t blocks = forward_blocks((a.T + kRows - 1) / kRows, once, two_turns);
+        const int64_t blocks = forward_blocks((a.T + kRows - 1) / kRows, once, forward_turns<T, S>(a.n, a.R != nullptr, window));
         const unsigned grid = static_cast<unsigned>(blocks < kMostBlocks ? blocks : kMostBlocks);
         const auto go = [&](auto win, auto add, auto stream) {
             forward_kernel<T, S, decltype(win)::value, decltype(add)::value, decltype(stream)::value><<<grid, S::B, 0, s>>>(a);
