@@ -116,3 +116,31 @@ def test_a_second_moment_that_is_not_zero_is_not_stored_as_zero():
         code, _ = adamw_ref.encode(x, t, "V")
         assert ((code == 0) == (x == 0)).all()
         assert (code[1:100] == 1).all()
+
+
+@pytest.mark.parametrize("alike", [False, True])
+def test_8_bit_moments_beside_fp32_ones(alike):
+    """How far they are apart over 750 steps after 750.  A step moves V by about a thousandth of itself, c, where codes lie
+    q <= V / 4 apart: it takes the next code with probability c / q, which adds c q to the variance, and loses 2 c of what
+    is there, so that it settles at q V / 2: a relative deviation of at most 8^-1/2 = 0.354, half of that for the root.
+    M's cut is off by at most q / 6^1/2, q <= M / 8, and 0.81 of its variance stays: 0.117.  Together 0.21 of an update."""
+    rng = np.random.default_rng(11)
+    n = 512
+    M, V = np.zeros(n, np.float32), np.zeros(n, np.float32)
+    codes = [(np.zeros(n, np.uint8), np.ones(n // 128, np.float32))] * 2
+    ratio, apart, size = [], 0.0, 0.0
+    g = (rng.normal(size=n) * 1e-3).astype(np.float32)
+    for t in range(1, 1501):
+        if not alike:
+            g = (rng.normal(size=n) * 1e-3).astype(np.float32)
+        m, v = adamw_ref.moments(g, 1.0, adamw_ref.decode(*codes[0], "M"), adamw_ref.decode(*codes[1], "V"), 0.9, 0.999)
+        codes = [adamw_ref.encode(m, t, "M"), adamw_ref.encode(v, t, "V")]
+        M, V = adamw_ref.moments(g, 1.0, M, V, 0.9, 0.999)
+        if t > 750:
+            ratio.append(adamw_ref.decode(*codes[1], "V") / V)
+            u8, u = (adamw_ref.update(np.zeros(n), a, b, 1.0, 0.9, 0.999, 1e-8, t, 0.0)[0] for a, b in ((m, v), (M, V)))
+            apart, size = apart + ((u8 - u) ** 2).sum(), size + (u ** 2).sum()
+    ratio = np.array(ratio)
+    assert ratio.std() < 8 ** -0.5
+    assert abs(ratio.mean() - 1) < 4 * 8 ** -0.5 / n ** 0.5  # the cut takes nothing on average: four deviations of a mean of n
+    assert np.sqrt(apart / size) < 0.21
