@@ -6,7 +6,7 @@
 // chunks of one combination of types lie together and take one launch.  A thread handles eight consecutive
 // elements, or four (twice, beside 8-bit moments) where an fp32 array is among those written; the 16 or 32 lanes that hold a block of 128
 // lie in one row of a wavefront or two, which exchange values without LDS.  Measured on large tensors: 6.0 TB/s
-// with fp32 moments (65.6M values of bf16 W and G: 240 us), 6.3 to 6.4 with 8-bit ones (262M: 415 to 422 us), 6.5
+// with fp32 moments (65.6M values of bf16 W and G: 240 us), 6.3 to 6.4 with 8-bit ones (262M: 415 to 424 us), 6.5
 // for the norm (262M bf16 gradients: 81 us); a step of 65 tensors of 4096 takes its kernel 3.5 us.
 #include "adam.hpp"
 #include "elem.hpp"
@@ -304,7 +304,10 @@ __device__ __forceinline__ void step_chunk(const Chunk& c, const AdamParams& p, 
 }
 
 // One chunk per workgroup.  The streaming hint only where every access is one whole piece: lines that two
-// lanes share are then read twice.
+// lanes share are then read twice.  At any size: between two steps of a model the arrays leave the cache.  With the hint and without,
+// us, three sets of arrays in turn: bf16 W and G, 8-bit moments 1M values 4.8 and 4.7, 4M 10.3 and 11.6, 34M 59.5 and 65.2; fp32
+// moments 1M 5.2 and 5.1, 4M 17.1 and 15.5, 17M 61.9 and 71.0, 67M 250 and 275.  What a step alone leaves in the cache and
+// repeats there is faster without (17M bf16, fp32 moments, one set 59.7 and 53.3).
 template <typename W, typename G, typename Moments>
 __global__ __launch_bounds__(kStepThreads<Moments>) void adamw_kernel(StepArgs a) {
     const Chunk c = a.chunks[blockIdx.x];
@@ -316,7 +319,8 @@ __global__ __launch_bounds__(kStepThreads<Moments>) void adamw_kernel(StepArgs a
     else step_chunk<false, W, G, Moments>(c, p, t, grad_scale);
 }
 
-// Workgroups that walk the chunks for the norm: 262M bf16 values 88.5 us, with 1024 of them 115, with 4096 92.6.
+// Workgroups that walk the chunks for the norm: 262M bf16 values 81.0 us, with 1024 of them 107, 1536 83.3, 4096 84.2; 66M fp32
+// ones 44.1, 49.9, 43.8, 44.4.
 constexpr int kNormBlocks = 2048;
 
 // A thread's part of the gradients of a chunk, as it lies in memory: eight bf16 values in a row (in the

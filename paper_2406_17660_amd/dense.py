@@ -14,7 +14,9 @@ NORMS = {"layer": grass.NORM_LAYER, "rms": grass.NORM_RMS}
 
 class NormLayer:
     """Layer norm or RMS norm over n features of up to T tokens, its parameters and their gradients (all
-    fp32), and what a backward pass needs of the forward pass before it."""
+    fp32), and what a backward pass needs of the forward pass before it: one forward pass, whose X (where
+    there is no R) is kept by reference and must not change until then; the next overwrites H, mean and rstd.  backward()
+    writes the parameters' gradients and does not add to them: sums over several batches are the caller's."""
 
     def __init__(self, n, T, dtype, kind="rms", bias=False, eps=1e-5, device="cuda"):
         self.n, self.T, self.kind, self.eps = n, T, NORMS[kind], eps
@@ -58,7 +60,8 @@ class AdamW:
     fp32: they cost nothing); of 128 consecutive elements, those whose gradients stay some 30000 times smaller than the
     largest ones' take steps that are too short.  weight_decay applies to matrices.  max_norm: the gradients' global
     norm is clipped to it, and a step whose
-    gradients are not finite changes nothing (t counts it all the same)."""
+    gradients are not finite changes nothing (t counts it all the same).  The gradients are to be written into the
+    same tensors each step: laying a plan out takes the host 2 us a tensor (300 of them 0.7 ms), much more than a step."""
 
     def __init__(self, parameters, adam=None, weight_decay=0.0, moments="f32", least_q8=4096, max_norm=None):
         assert moments in ("f32", "q8")
