@@ -381,7 +381,7 @@ __global__ __launch_bounds__(kSumWaves* kWave) void column_sums_kernel(const flo
 // bf16 30519 x 5461 226 / 191, 1525 x 5461 18.2 / 19.7, in windows 11904 x 4200 59.9 / 60.9, fp32 37810 x 2204 195 / 177, 1890 x 2204
 // 13.9 / 14.9: where the call streams and its rows are fp32 or start anywhere.
 template <typename T>
-bool three_vectors(int tpr, bool streamed, bool window, bool on_words, bool add) {
+constexpr bool three_vectors(int tpr, bool streamed, bool window, bool on_words, bool add) {
     if (tpr == 64) return sizeof(T) == 2 && (!add || !on_words);
     return tpr == 128 || (streamed && (sizeof(T) == 4 || !window));
 }
@@ -434,8 +434,10 @@ int launch(BackwardArgs a, hipStream_t s) {
             blocks = rows_too ? blocks_of(a.T, S::B / S::TPR) : 0;
             const unsigned row_blocks = static_cast<unsigned>(blocks);
             const auto go = [&](auto win, auto add, auto stream) {
-                backward_kernel<T, S, decltype(win)::value, decltype(add)::value, decltype(stream)::value>
-                    <<<column_blocks + row_blocks, S::B, 0, s>>>(a);
+                constexpr bool kWindow = decltype(win)::value, kAdd = decltype(add)::value, kOnce = decltype(stream)::value;
+                // (windows start on words; kernels that the rule leaves without calls are not built)
+                if constexpr (S::V != 3 || S::TPR == 512 || three_vectors<T>(S::TPR, kOnce, kWindow, kWindow, kAdd))
+                    backward_kernel<T, S, kWindow, kAdd, kOnce><<<column_blocks + row_blocks, S::B, 0, s>>>(a);
             };
             const auto with_add = [&](auto win, auto add) { once ? go(win, add, std::true_type{}) : go(win, add, std::false_type{}); };
             const auto with_window = [&](auto win) { a.dR ? with_add(win, std::true_type{}) : with_add(win, std::false_type{}); };

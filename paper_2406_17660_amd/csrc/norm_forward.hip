@@ -272,6 +272,14 @@ int forward_turns(int64_t n, bool add, bool window) {
     return two && S::TPR <= kWave && n * sizeof(T) * 8 >= S::TPR * S::V * 16 * 5 ? 4 : 16;
 }
 
+// Three vectors a thread put more rows into a workgroup.  With R, two / three us: rows of 64 lanes 2320 x 1293 bf16 8.8 / 9.9,
+// 6050 x 1033 14.5 / 12.5, so from two workgroups per compute unit (`many`) on; wider ones 3038 x 2057 14.5 / 15.0, 1249 x 5001
+// 12.7 / 13.6, 60768 x 2057 242 / 222, 24995 x 5001 233 / 199, so where the call streams.  Without R at any number of rows: 5808 x 1033
+// 9.6 / 8.1, 242013 x 1033 258 / 204, 12019 x 520 fp32 11.6 / 8.6; rows of 128 and 256 lanes win and lose a tenth by how many turns are left.
+constexpr bool three_vectors(int tpr, bool add, bool streamed, bool many) {
+    return !add || (tpr == 64 ? many : streamed);
+}
+
 template <typename T>
 void launch(const ForwardArgs& a, hipStream_t s) {
     if (!in_registers<T>(a.n)) {
@@ -282,11 +290,7 @@ void launch(const ForwardArgs& a, hipStream_t s) {
     const bool window = a.n * sizeof(T) % 16 == 0 && on16(a.X, a.ldx) && on16(a.Y, a.ldy) &&
                         (!a.R || (on16(a.R, a.ldr) && on16(a.H, a.ldh)));
     const bool once = static_cast<double>(a.T) * a.n * sizeof(T) * (a.R ? 4 : 2) > kStreamed;
-    // Three vectors a thread put more rows into a workgroup.  With R, two / three us: rows of 64 lanes 2320 x 1293 bf16 8.8 / 9.9,
-    // 6050 x 1033 14.5 / 12.5, so from two workgroups per compute unit on; wider ones 3038 x 2057 14.5 / 15.0, 1249 x 5001 12.7 / 13.6,
-    // 60768 x 2057 242 / 222, 24995 x 5001 233 / 199, so where the call streams.  Without R at any number of rows: 5808 x 1033 9.6 / 8.1,
-    // 242013 x 1033 258 / 204, 12019 x 520 fp32 11.6 / 8.6; rows of 128 and 256 lanes win and lose a tenth by how many turns are left.
-    const auto three = [&](int tpr) { return !a.R || (tpr == 64 ? a.T >= 2 * kUnits * (512 / tpr) : once); };
+    const auto three = [&](int tpr) { return three_vectors(tpr, a.R != nullptr, once, a.T >= 2 * kUnits * (512 / tpr)); };
     by_shape<T>(a.n, three, [&](auto shape) {
         typedef decltype(shape) S;
         constexpr int64_t kRows = S::B / S::TPR;
@@ -294,7 +298,10 @@ void launch(const ForwardArgs& a, hipStream_t s) {
         const int64_t blocks = forward_blocks((a.T + kRows - 1) / kRows, once, forward_turns<T, S>(a.n, a.R != nullptr, window));
         const unsigned grid = static_cast<unsigned>(blocks < kMostBlocks ? blocks : kMostBlocks);
         const auto go = [&](auto win, auto add, auto stream) {
-            forward_kernel<T, S, decltype(win)::value, decltype(add)::value, decltype(stream)::value><<<grid, S::B, 0, s>>>(a);
+            constexpr bool kAdd = decltype(add)::value, kOnce = decltype(stream)::value;
+            // (kernels that the rule leaves without calls are not built)
+            if constexpr (S::V != 3 || S::TPR == 512 || three_vectors(S::TPR, kAdd, kOnce, true))
+                forward_kernel<T, S, decltype(win)::value, kAdd, kOnce><<<grid, S::B, 0, s>>>(a);
         };
         const auto with_add = [&](auto win, auto add) { once ? go(win, add, std::true_type{}) : go(win, add, std::false_type{}); };
         const auto with_window = [&](auto win) { a.R ? with_add(win, std::true_type{}) : with_add(win, std::false_type{}); };
