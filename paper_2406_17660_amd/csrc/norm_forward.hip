@@ -261,7 +261,7 @@ int64_t forward_blocks(int64_t groups, bool once, int turns) {
 // turn.  TB/s at 1.2 GB with 2, 4 and 16 turns.  fp32: 512 values 5.98 5.94 5.59, 4096 6.18 6.05 6.01, 3001 5.42 5.41 5.13,
 // with R 512 5.96 5.74 5.56.  bf16 with R: 512 5.98 5.68 5.30, 4096 6.02 5.76 5.88, 200 5.51 5.29 4.65, 500 (no window) 5.22 4.91 4.37,
 // 2601 (no window) 3.99 4.33 4.97.  bf16 without: 512 5.83 6.11 5.38, 2048 6.11 6.08 5.83, 200 4.98 5.33 4.97, 501 5.02 5.16 4.54,
-// 2601 3.74 4.09 4.76, 2200 (three vectors) 4.17 4.69 5.27; 64, which half of a row's lanes have no part of, 3.48 3.90 4.23 (80, with
+// 2601 3.74 4.09 4.76, 2200 (three vectors) 4.17 4.69 5.27; 64, which half of a row's lanes have no part of, 3.48 3.90 4.34 (80, with
 // five eighths at work, 4.21 4.44 3.99 at 180 MB and 4.16 4.75 4.94).
 template <typename T, typename S>
 int forward_turns(int64_t n, bool add, bool window) {
