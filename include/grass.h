@@ -1,6 +1,6 @@
 /*
- * grass.h - C ABI of the GRASS structured-sparse gradient step for one linear layer, and of the norms
- *           and the AdamW step around it, on one AMD MI355X (gfx950).
+ * grass.h - C ABI of the GRASS structured-sparse gradient step for one linear layer, and of the norms,
+ *           the embedding, the log probabilities and the AdamW step around it, on one AMD MI355X (gfx950).
  *
  * Notation (paper, Sections 2 and 3.1): a linear layer has weight W (m x n), input
  * activations X (T x n) and output gradient dY (T x m), T being the token batch
@@ -41,7 +41,8 @@
  *   - Index arrays (idx) live in device memory, so their VALUES cannot be validated
  *     before the launch: every entry must lie inside the dimension it indexes
  *     (grass_select_rows writes such arrays).  Entries outside it make the kernels
- *     read or write outside the caller's buffers.
+ *     read or write outside the caller's buffers.  (Token numbers, `ids` and `targets`, are checked
+ *     by the kernels.)
  *   - No call records a memset or an event (the _timed call excepted) or allocates, so
  *     calls can be captured into a HIP graph.
  */
@@ -567,6 +568,77 @@ grass_status grass_adamw_step_scalars(float lr, float beta1, float beta2, int64_
 size_t grass_grad_norm_workspace(const grass_adamw_layout* layout);
 grass_status grass_grad_norm(const void* plan, const grass_adamw_layout* layout, float max_norm,
                              float* out, void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * The two ends of a model: the embedding lookup that the first layer reads, and the log probabilities
+ * that the loss is made of, with their gradients (dE and, through the head, its weights' gradient are what
+ * grass_adamw_step takes).  Token numbers are 32 or 64 bits wide (`idt`) and, unlike the other calls'
+ * index arrays, may hold any value: one outside 0 .. V - 1, such as the -1 or -100 that stands for
+ * padding, names no token.
+ *
+ * Lookup:  Y[t, :] = scale * E[ids[t], :], rounded once to `ydt`; zeros where ids[t] names no token.
+ * E: V x n of dtype `edt`, Y: T x n, each with a leading dimension of its own; they do not overlap.  T = 0 is
+ * a no-op; V, n >= 1; scale is finite.
+ * Errors: NULL, SHAPE (also an address that is not a multiple of its type's size), DTYPE. */
+typedef enum { GRASS_I32 = 0, GRASS_I64 = 1 } grass_index;
+grass_status grass_embed_forward(const void* E, grass_dtype edt, int64_t V, int64_t n, int64_t lde,
+                                 const void* ids, grass_index idt, int64_t T, float scale, void* Y,
+                                 grass_dtype ydt, int64_t ldy, void* stream);
+
+/* Its gradient:  dE[v, :] = scale * sum over the t with ids[t] = v of dY[t, :]   (+ dE[v, :] where
+ * accumulate is not 0, as after the gradient of a head that shares the weights), rounded once to `gdt`.
+ * dY: T x n of dtype `dt`; dE: V x n of dtype `gdt`; they do not overlap.  Rows of tokens that do not
+ * occur are zeros, or with accumulate neither read nor written; rows of dY whose ids[t] names no token are
+ * not read.  The sums are fp32, in an order that depends on the token numbers and sizes alone, so
+ * that equal calls give equal bits.  `ws` must hold grass_embed_backward_workspace(T, V, n) bytes,
+ * 16-byte aligned.  T = 0 writes zeros, or with accumulate nothing; V, n >= 1; scale is finite.
+ * Errors: NULL, SHAPE (also an address that is not a multiple of its type's size), DTYPE, WORKSPACE. */
+size_t grass_embed_backward_workspace(int64_t T, int64_t V, int64_t n);
+grass_status grass_embed_backward(const void* dY, grass_dtype dt, int64_t lddy, const void* ids,
+                                  grass_index idt, int64_t T, int64_t V, int64_t n, float scale,
+                                  int accumulate, void* dE, grass_dtype gdt, int64_t ldde, void* ws,
+                                  size_t ws_bytes, void* stream);
+
+/* Log probabilities of given tokens.  For every row x of `logits` (T x V of dtype `dt`), with the
+ * logits multiplied by `scale` (the inverse of a temperature; finite, above 0):
+ *   rmax[t] = max_j x_j       rlog[t] = log sum_j exp(scale * (x_j - rmax))
+ *   log p_j = scale * (x_j - rmax) - rlog
+ *   logp[t] = log p_j of j = targets[t]; 0 where targets[t] names no token
+ *   entropy[t] = -sum_j p_j log p_j
+ *   top_idx[t, 0 .. top - 1], top_logp[t, 0 .. top - 1]: the tokens of the largest logits in falling order,
+ *   ties by the lower token, and their log probabilities (T x top each, without gaps)
+ * all fp32 but top_idx; each output may be NULL where it is not wanted (targets and logp together,
+ * top_logp and top_idx together with top = 0).  rmax and rlog are for the backward pass.
+ * Logits of minus infinity are masked: their p is 0, and no alternative is one of them: where fewer than `top`
+ * logits are left, the rest of top_idx is -1 and of top_logp minus infinity.  A row that is all masked
+ * has logp minus infinity, entropy 0, rmax minus infinity and rlog 0.  In a row with a NaN or with plus
+ * infinity rlog, entropy, logp (where the target names a token) and top_logp are NaN, and top_idx is
+ * -1; other rows are not affected.
+ * 0 <= top <= GRASS_LOGP_MOST_TOP and top <= V.  `ws` must hold grass_logp_forward_workspace(T, V, top,
+ * dt) bytes, 16-byte aligned (NULL where that is 0).  Equal calls give equal bits.  T = 0 is a no-op; V >= 1.
+ * Errors: NULL (also one of a pair without the other), SHAPE (also an address that is not a multiple
+ * of its type's size), DTYPE, WORKSPACE. */
+#define GRASS_LOGP_MOST_TOP 64
+size_t grass_logp_forward_workspace(int64_t T, int64_t V, int64_t top, grass_dtype dt);
+grass_status grass_logp_forward(const void* logits, grass_dtype dt, int64_t T, int64_t V, int64_t ldl,
+                                const void* targets, grass_index idt, float scale, float* logp,
+                                float* entropy, float* rmax, float* rlog, int64_t top,
+                                float* top_logp, int32_t* top_idx, void* ws, size_t ws_bytes,
+                                void* stream);
+
+/* Its gradient, from the logits and what the forward pass kept (same `scale`):
+ *   dlogits[t, j] = scale * (dlogp[t] * ([j = targets[t]] - p_j) - dentropy[t] * p_j * (log p_j + entropy[t]))
+ * rounded once to `dt`.  dlogp, dentropy: T floats, the gradients of logp and entropy; NULL: zeros (targets
+ * may then be NULL, too; entropy is read only beside dentropy).  A row whose target names no token takes no
+ * part in the first term.  A row without either term (dentropy[t] and dlogp[t] 0, or no token) is
+ * zeros and is not read, whatever it holds; a row that is all masked is zeros.
+ * dlogits may be logits (the same address and leading dimension); other overlaps are not allowed.
+ * T = 0 is a no-op; V >= 1.
+ * Errors: NULL, SHAPE (also an address that is not a multiple of its type's size), DTYPE. */
+grass_status grass_logp_backward(const void* logits, grass_dtype dt, int64_t T, int64_t V, int64_t ldl,
+                                 const void* targets, grass_index idt, float scale, const float* rmax,
+                                 const float* rlog, const float* dlogp, const float* entropy,
+                                 const float* dentropy, void* dlogits, int64_t lddl, void* stream);
 
 /* ---------------------------------------------------------------------------
  * Test hooks.  The launchers choose their kernels from the shapes and alignments of a call;

@@ -3,6 +3,7 @@
 // that fails validation has no side effect (and can be exercised on a machine without a
 // GPU).
 #include <atomic>
+#include <cmath>
 #include <initializer_list>
 
 #include "common.hpp"
@@ -529,6 +530,102 @@ grass_status grass_norm_backward(grass_norm kind, const void* dY, int64_t lddy, 
     if (need > 0 && (!ws || ws_bytes < need || !aligned_to(ws, 4))) return GRASS_ERR_WORKSPACE;
     return launch_norm_backward(kind, dY, lddy, H, ldh, dR, lddr, dt, T, n, gain, gdt, mean, rstd, dX, lddx, dgain,
                                 dbias, ws, as_stream(stream));
+}
+
+// Token numbers of T tokens: width, address, and that it is a multiple of their size.
+static grass_status check_tokens(const void* ids, grass_index idt, int64_t T) {
+    if (idt != GRASS_I32 && idt != GRASS_I64) return GRASS_ERR_DTYPE;
+    if (!present(ids, T)) return GRASS_ERR_NULL;
+    return aligned_to(ids, idt == GRASS_I64 ? 8 : 4) ? GRASS_OK : GRASS_ERR_SHAPE;
+}
+
+static grass_status check_embed(int64_t T, int64_t V, int64_t n, float scale, grass_dtype rows, grass_dtype weights) {
+    if (T < 0 || V < 1 || n < 1 || !small(T) || !small(V) || !small(n) || !std::isfinite(scale)) return GRASS_ERR_SHAPE;
+    return dtype_ok(rows) && dtype_ok(weights) ? GRASS_OK : GRASS_ERR_DTYPE;
+}
+
+grass_status grass_embed_forward(const void* E, grass_dtype edt, int64_t V, int64_t n, int64_t lde,
+                                 const void* ids, grass_index idt, int64_t T, float scale, void* Y,
+                                 grass_dtype ydt, int64_t ldy, void* stream) {
+    grass_status st = check_embed(T, V, n, scale, ydt, edt);
+    if (st == GRASS_OK) st = check_tokens(ids, idt, T);
+    if (st != GRASS_OK) return st;
+    if (lde < n || ldy < n) return GRASS_ERR_SHAPE;
+    if (!present(E, T) || !present(Y, T)) return GRASS_ERR_NULL;
+    if (!on_elements(edt, {E}) || !on_elements(ydt, {Y})) return GRASS_ERR_SHAPE;
+    return launch_embed_forward(E, edt, V, n, lde, ids, idt, T, scale, Y, ydt, ldy, as_stream(stream));
+}
+
+size_t grass_embed_backward_workspace(int64_t T, int64_t V, int64_t n) {
+    if (check_embed(T, V, n, 1.f, GRASS_F32, GRASS_F32) != GRASS_OK) return 0;
+    return embed_backward_workspace_bytes(T, V, n);
+}
+
+grass_status grass_embed_backward(const void* dY, grass_dtype dt, int64_t lddy, const void* ids,
+                                  grass_index idt, int64_t T, int64_t V, int64_t n, float scale,
+                                  int accumulate, void* dE, grass_dtype gdt, int64_t ldde, void* ws,
+                                  size_t ws_bytes, void* stream) {
+    grass_status st = check_embed(T, V, n, scale, dt, gdt);
+    if (st == GRASS_OK) st = check_tokens(ids, idt, T);
+    if (st != GRASS_OK) return st;
+    if (lddy < n || ldde < n) return GRASS_ERR_SHAPE;
+    if (!present(dY, T) || !dE) return GRASS_ERR_NULL;
+    if (!on_elements(dt, {dY}) || !on_elements(gdt, {dE})) return GRASS_ERR_SHAPE;
+    const size_t need = embed_backward_workspace_bytes(T, V, n);
+    if (need > 0 && (!ws || ws_bytes < need || !aligned_to(ws, 16))) return GRASS_ERR_WORKSPACE;
+    return launch_embed_backward(dY, dt, lddy, ids, idt, T, V, n, scale, accumulate != 0, dE, gdt, ldde, ws,
+                                 as_stream(stream));
+}
+
+static grass_status check_logp(int64_t T, int64_t V, grass_dtype dt) {
+    if (T < 0 || V < 1 || !small(T) || !small(V)) return GRASS_ERR_SHAPE;
+    return dtype_ok(dt) ? GRASS_OK : GRASS_ERR_DTYPE;
+}
+
+size_t grass_logp_forward_workspace(int64_t T, int64_t V, int64_t top, grass_dtype dt) {
+    if (check_logp(T, V, dt) != GRASS_OK || top < 0 || top > GRASS_LOGP_MOST_TOP || top > V) return 0;
+    return logp_forward_workspace_bytes(T, V, top, dt);
+}
+
+grass_status grass_logp_forward(const void* logits, grass_dtype dt, int64_t T, int64_t V, int64_t ldl,
+                                const void* targets, grass_index idt, float scale, float* logp,
+                                float* entropy, float* rmax, float* rlog, int64_t top,
+                                float* top_logp, int32_t* top_idx, void* ws, size_t ws_bytes,
+                                void* stream) {
+    grass_status st = check_logp(T, V, dt);
+    if (st != GRASS_OK) return st;
+    if (ldl < V || top < 0 || top > GRASS_LOGP_MOST_TOP || top > V || !(scale > 0.f) || !std::isfinite(scale))
+        return GRASS_ERR_SHAPE;
+    if (T > 0 && ((targets == nullptr) != (logp == nullptr) || (top > 0) != (top_logp != nullptr) || (top > 0) != (top_idx != nullptr)))
+        return GRASS_ERR_NULL;
+    if (!present(logits, T)) return GRASS_ERR_NULL;
+    if (targets) st = check_tokens(targets, idt, T);
+    if (st != GRASS_OK) return st;
+    if (!on_elements(dt, {logits}) || !on_elements(GRASS_F32, {logp, entropy, rmax, rlog, top_logp, top_idx}))
+        return GRASS_ERR_SHAPE;
+    const size_t need = logp_forward_workspace_bytes(T, V, top, dt);
+    if (need > 0 && (!ws || ws_bytes < need || !aligned_to(ws, 16))) return GRASS_ERR_WORKSPACE;
+    return launch_logp_forward(logits, dt, T, V, ldl, targets, idt, scale, logp, entropy, rmax, rlog, top, top_logp,
+                               top_idx, ws, as_stream(stream));
+}
+
+grass_status grass_logp_backward(const void* logits, grass_dtype dt, int64_t T, int64_t V, int64_t ldl,
+                                 const void* targets, grass_index idt, float scale, const float* rmax,
+                                 const float* rlog, const float* dlogp, const float* entropy,
+                                 const float* dentropy, void* dlogits, int64_t lddl, void* stream) {
+    grass_status st = check_logp(T, V, dt);
+    if (st != GRASS_OK) return st;
+    if (ldl < V || lddl < V || !(scale > 0.f) || !std::isfinite(scale)) return GRASS_ERR_SHAPE;
+    if (dlogp || targets) st = check_tokens(targets, idt, T);
+    if (st != GRASS_OK) return st;
+    if (!present(logits, T) || !present(rmax, T) || !present(rlog, T) || !present(dlogits, T) ||
+        (dentropy && !present(entropy, T)))
+        return GRASS_ERR_NULL;
+    if (!on_elements(dt, {logits, dlogits}) ||
+        !on_elements(GRASS_F32, {rmax, rlog, dlogp, dentropy ? entropy : nullptr, dentropy}))
+        return GRASS_ERR_SHAPE;
+    return launch_logp_backward(logits, dt, T, V, ldl, targets, idt, scale, rmax, rlog, dlogp, entropy, dentropy, dlogits,
+                                lddl, as_stream(stream));
 }
 
 static grass_status check_adamw_tensors(int count, const grass_adamw_tensor* tensors) {

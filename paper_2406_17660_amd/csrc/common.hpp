@@ -300,6 +300,24 @@ grass_status launch_norm_backward(grass_norm kind, const void* dY, int64_t lddy,
                                   const void* gain, grass_dtype gdt, const float* mean, const float* rstd,
                                   void* dX, int64_t lddx, float* dgain, float* dbias, void* ws, hipStream_t s);
 
+// The embedding lookup and its gradient by tokens.
+grass_status launch_embed_forward(const void* E, grass_dtype edt, int64_t V, int64_t n, int64_t lde, const void* ids,
+                                  grass_index idt, int64_t T, float scale, void* Y, grass_dtype ydt, int64_t ldy,
+                                  hipStream_t s);
+size_t embed_backward_workspace_bytes(int64_t T, int64_t V, int64_t n);
+grass_status launch_embed_backward(const void* dY, grass_dtype dt, int64_t lddy, const void* ids, grass_index idt, int64_t T,
+                                   int64_t V, int64_t n, float scale, bool accumulate, void* dE, grass_dtype gdt,
+                                   int64_t ldde, void* ws, hipStream_t s);
+
+// Log probabilities of given tokens and their gradient.
+size_t logp_forward_workspace_bytes(int64_t T, int64_t V, int64_t top, grass_dtype dt);
+grass_status launch_logp_forward(const void* logits, grass_dtype dt, int64_t T, int64_t V, int64_t ldl, const void* targets,
+                                 grass_index idt, float scale, float* logp, float* entropy, float* rmax, float* rlog,
+                                 int64_t top, float* top_logp, int32_t* top_idx, void* ws, hipStream_t s);
+grass_status launch_logp_backward(const void* logits, grass_dtype dt, int64_t T, int64_t V, int64_t ldl, const void* targets,
+                                  grass_index idt, float scale, const float* rmax, const float* rlog, const float* dlogp,
+                                  const float* entropy, const float* dentropy, void* dlogits, int64_t lddl, hipStream_t s);
+
 // AdamW over many tensors and the norm of their gradients.  The tensors have been checked; the
 // number of chunks that a plan of them has, by group, and the plan itself.
 void adamw_count(int count, const grass_adamw_tensor* tensors, grass_adamw_layout* layout);

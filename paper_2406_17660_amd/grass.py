@@ -24,6 +24,8 @@ TEST_GEMM_TILE, TEST_FUSED_STATS, TEST_PACK_MXT, TEST_NO_PAIRS, TEST_MAX_K_SLICE
 TEST_NO_NARROW_GATHER, TEST_RUN_TILE, TEST_UNALIGNED_X = 5, 6, 7
 CALL_CGRAD, CALL_STEP, CALL_DENSE = range(3)
 NORM_LAYER, NORM_RMS = 0, 1
+I32, I64 = 0, 1
+LOGP_MOST_TOP = 64
 MOMENTS_F32, MOMENTS_Q8 = 0, 1
 MOMENTS_BLOCK = 128  # elements of an 8-bit moment that share a scale
 (KERNEL_NONE, KERNEL_128_STAGED, KERNEL_128, KERNEL_128_256, KERNEL_256, KERNEL_256_ROWS, KERNEL_256_UNALIGNED,
@@ -46,6 +48,8 @@ EXPORTS = [
     "grass_norm_forward", "grass_norm_backward_workspace", "grass_norm_backward",
     "grass_adamw_plan_bytes", "grass_adamw_plan", "grass_adamw_step", "grass_adamw_step_scalars",
     "grass_grad_norm_workspace", "grass_grad_norm",
+    "grass_embed_forward", "grass_embed_backward_workspace", "grass_embed_backward",
+    "grass_logp_forward_workspace", "grass_logp_forward", "grass_logp_backward",
 ]
 
 _lib = None
@@ -155,6 +159,14 @@ def lib():
     L.grass_grad_norm_workspace.argtypes = [layout]
     L.grass_grad_norm_workspace.restype = sz
     L.grass_grad_norm.argtypes = [vp, layout, f32, vp, vp, sz, vp]
+    L.grass_embed_forward.argtypes = [vp, i32, i64, i64, i64, vp, i32, i64, f32, vp, i32, i64, vp]
+    L.grass_embed_backward_workspace.argtypes = [i64, i64, i64]
+    L.grass_embed_backward_workspace.restype = sz
+    L.grass_embed_backward.argtypes = [vp, i32, i64, vp, i32, i64, i64, i64, f32, i32, vp, i32, i64, vp, sz, vp]
+    L.grass_logp_forward_workspace.argtypes = [i64, i64, i64, i32]
+    L.grass_logp_forward_workspace.restype = sz
+    L.grass_logp_forward.argtypes = [vp, i32, i64, i64, i64, vp, i32, f32, vp, vp, vp, vp, i64, vp, vp, vp, sz, vp]
+    L.grass_logp_backward.argtypes = [vp, i32, i64, i64, i64, vp, i32, f32, vp, vp, vp, vp, vp, vp, i64, vp]
     for name in EXPORTS:
         if name not in ("grass_status_string", "grass_select_workspace", "grass_cgrad_workspace",
                         "grass_select_static_capacity",
@@ -162,7 +174,8 @@ def lib():
                         "grass_cgrad_group_workspace", "grass_step_group_workspace",
                         "grass_step_cols_workspace", "grass_test_least_workspace",
                         "grass_norm_backward_workspace", "grass_adamw_plan_bytes",
-                        "grass_grad_norm_workspace"):
+                        "grass_grad_norm_workspace", "grass_embed_backward_workspace",
+                        "grass_logp_forward_workspace"):
             getattr(L, name).restype = i32
     L.grass_test_product_us.argtypes = [i32, i32, i64, i64]
     L.grass_test_product_us.restype = C.c_double
@@ -765,6 +778,102 @@ def grad_norm(plan, max_norm, out, ws):
     _check(lib().grass_grad_norm(plan.plan.data_ptr(), C.byref(plan.layout), max_norm, out.data_ptr(), wp, wb,
                                  _stream()), "grass_grad_norm")
     return out
+
+
+_INDEXES = {torch.int32: I32, torch.int64: I64}
+
+
+def _tokens(t, T):
+    """(address, type) of T token numbers."""
+    assert t.is_cuda and t.shape == (T,) and t.is_contiguous(), "token numbers: one contiguous vector"
+    code = _INDEXES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"unsupported type of token numbers {t.dtype}")
+    return t.data_ptr(), code
+
+
+def _here(*tensors):
+    """Refuses tensors of another device than the current one, whose stream a call is issued on."""
+    device = torch.cuda.current_device() if _device is None else _device()
+    for t in tensors:
+        assert t is None or t.get_device() == device, "tensors of the current device expected"
+
+
+def _rows(t):
+    """(address, rows, cols, leading dimension) of a device matrix whose rows, a single one too, are contiguous."""
+    rows, cols = t.shape
+    ld, step = t.stride()
+    assert t.is_cuda and (step == 1 or cols <= 1), "rows must be contiguous"
+    return t.data_ptr(), rows, cols, cols if rows <= 1 else ld
+
+
+def embed_forward(E, ids, Y, scale=1.0):
+    """Y[t, :] = scale * E[ids[t], :]; rows of zeros where ids[t] is outside the vocabulary."""
+    _here(E, ids, Y)
+    pE, V, n, lde = _rows(E)
+    pY, T, ny, ldy = _rows(Y)
+    assert ny == n, "shapes differ"
+    pi, idt = _tokens(ids, T)
+    _check(lib().grass_embed_forward(pE, _dtype(E), V, n, lde, pi, idt, T, scale, pY, _dtype(Y), ldy, _stream()),
+           "grass_embed_forward")
+    return Y
+
+
+def embed_backward_workspace(T, V, n) -> int:
+    return int(lib().grass_embed_backward_workspace(T, V, n))
+
+
+def embed_backward(dY, ids, dE, ws, scale=1.0, accumulate=False):
+    """dE[v, :] = scale * (sum of the rows of dY whose token is v), added to what dE holds where accumulate is true."""
+    _here(dY, ids, dE, ws)
+    pY, T, n, lddy = _rows(dY)
+    pE, V, ne, ldde = _rows(dE)
+    assert ne == n, "shapes differ"
+    pi, idt = _tokens(ids, T)
+    wp, wb = _ws(ws)
+    _check(lib().grass_embed_backward(pY, _dtype(dY), lddy, pi, idt, T, V, n, scale, int(bool(accumulate)), pE, _dtype(dE),
+                                      ldde, wp, wb, _stream()), "grass_embed_backward")
+    return dE
+
+
+def logp_forward_workspace(T, V, top, dtype) -> int:
+    return int(lib().grass_logp_forward_workspace(T, V, top, dtype))
+
+
+def logp_forward(logits, targets, logp, ws, scale=1.0, entropy=None, rmax=None, rlog=None, top_logp=None, top_idx=None):
+    """Log probabilities of the targets under the logits' rows (targets and logp: None where not wanted), the rows'
+    entropies, what the backward pass needs of them (rmax, rlog: T floats), and the alternatives of largest
+    probability with their log probabilities (top_idx int32, top_logp: T x top)."""
+    _here(logits, targets, logp, ws, entropy, rmax, rlog, top_logp, top_idx)
+    pl, T, V, ldl = _rows(logits)
+    f32 = torch.float32
+    pt, idt = (None, I32) if targets is None else _tokens(targets, T)
+    plogp, pent, pmax, plog = (None if v is None else _vector(v, T, f32) for v in (logp, entropy, rmax, rlog))
+    top, ptl, pti = 0, None, None
+    if top_idx is not None:
+        top = top_idx.shape[1]
+        assert top_idx.shape == top_logp.shape == (T, top) and top_idx.dtype is torch.int32 and top_logp.dtype is f32
+        assert top_idx.is_cuda and top_logp.is_cuda and top_idx.is_contiguous() and top_logp.is_contiguous()
+        if top:
+            ptl, pti = top_logp.data_ptr(), top_idx.data_ptr()
+    wp, wb = _ws(ws)
+    _check(lib().grass_logp_forward(pl, _dtype(logits), T, V, ldl, pt, idt, scale, plogp, pent, pmax, plog, top, ptl, pti, wp,
+                                    wb, _stream()), "grass_logp_forward")
+    return logp
+
+
+def logp_backward(logits, targets, rmax, rlog, dlogp, dlogits, scale=1.0, entropy=None, dentropy=None):
+    """The gradient of the logits from those of logp and entropy (None: zeros); dlogits may be logits."""
+    _here(logits, targets, rmax, rlog, dlogp, dlogits, entropy, dentropy)
+    pl, T, V, ldl = _rows(logits)
+    pd, Td, Vd, lddl = _rows(dlogits)
+    assert (Td, Vd) == (T, V) and dlogits.dtype is logits.dtype, "shapes or types differ"
+    f32 = torch.float32
+    pt, idt = (None, I32) if targets is None else _tokens(targets, T)
+    pmax, plog, pdlogp, pent, pdent = (None if v is None else _vector(v, T, f32) for v in (rmax, rlog, dlogp, entropy, dentropy))
+    _check(lib().grass_logp_backward(pl, _dtype(logits), T, V, ldl, pt, idt, scale, pmax, plog, pdlogp, pent, pdent, pd, lddl,
+                                     _stream()), "grass_logp_backward")
+    return dlogits
 
 
 def workspace(nbytes: int, device="cuda"):
