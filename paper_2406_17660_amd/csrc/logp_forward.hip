@@ -1,102 +1,416 @@
 // grass_logp_forward: log probabilities of given tokens, entropies and alternatives.
+//
+// Bound by memory: a row is read once and stays in the registers of the threads that share it, for its maximum, its
+// sums and its alternatives.  With c = scale log2(e) and d = (x - rmax) c, s = sum 2^d and u = sum 2^d d give
+// rlog = ln s and entropy = ln s - ln(2) u / s.
 #include "elem.hpp"
 #include "tokens.hpp"
 
 namespace grass {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr float kLog2e = 1.44269504088896f, kLn2 = 0.693147180559945f;
 
 struct ForwardArgs {
     const void* logits;
     int64_t T, ldl;
-    int V, top;
+    int V, top, parts;
     Tokens targets;
     float scale;
     float *logp, *entropy, *rmax, *rlog, *top_logp;
     int32_t* top_idx;
+    // of rows in parts: maximum, s and u of each part, and its alternatives
+    float4* part;
+    uint64_t* part_top;
 };
 
-// Numbers in the order of the logits (both zeros alike); below them 0.
+// Numbers in the order of the logits (both zeros alike), above 0; and the logit again.
 __device__ __forceinline__ uint32_t order_of(float x) {
     const uint32_t u = __float_as_uint(x + 0.f);
     return (u >> 31) ? ~u : u | 0x80000000u;
 }
-
-// Largest of a workgroup's values, for every thread.
-template <typename N, typename F>
-__device__ __forceinline__ N over_block(N v, F f) {
-    __shared__ N part[kThreads / kWave];
-    for (int o = kWave / 2; o > 0; o >>= 1) v = f(v, __shfl_xor(v, o, kWave));
-    __syncthreads();
-    if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = v;
-    __syncthreads();
-    v = part[0];
-    for (int w = 1; w < kThreads / kWave; ++w) v = f(v, part[w]);
-    return v;
+__device__ __forceinline__ float logit_of(uint32_t order) {
+    return __uint_as_float((order >> 31) ? order & 0x7FFFFFFFu : ~order);
+}
+// An alternative: in the order of the logits, then of the tokens, the lower one first.
+__device__ __forceinline__ uint64_t key_of(uint32_t order, int token) {
+    return static_cast<uint64_t>(order) << 32 | static_cast<uint32_t>(~token);
 }
 
-// One row per workgroup at a time: a pass over it for the maximum, one for the sums, one for each alternative.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void forward_kernel(ForwardArgs a) {
-    for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x) {
-        const T* x = static_cast<const T*>(a.logits) + t * a.ldl;
-        float m = -INFINITY;
-        for (int c = threadIdx.x; c < a.V; c += kThreads) m = fmaxf(m, load_as_f32(x + c));
-        m = over_block(m, [](float p, float q) { return fmaxf(p, q); });
-        const float m0 = m == -INFINITY ? 0.f : m;
-        float sum = 0.f, mean = 0.f;
-        for (int c = threadIdx.x; c < a.V; c += kThreads) {
-            const float d = scaled_difference(load_as_f32(x + c), m0, a.scale), e = expf(d);
-            sum += e;
-            if (e > 0.f) mean += e * d;
-        }
-        const auto add = [](float p, float q) { return p + q; };
-        sum = over_block(sum, add);
-        mean = over_block(mean, add);
-        const bool none = sum == 0.f;
-        const float log = none ? 0.f : logf(sum);
-        if (threadIdx.x == 0) {
-            if (a.rmax) a.rmax[t] = m;
-            if (a.rlog) a.rlog[t] = log;
-            if (a.entropy) a.entropy[t] = none ? 0.f : log - mean / sum;
-            if (a.logp) {
-                const uint32_t j = a.targets[t];
-                a.logp[t] = j < a.targets.V ? scaled_difference(load_as_f32(x + j), m0, a.scale) - log : 0.f;
+// The largest of three.  (As a builtin, each operand from memory is first made a quiet NaN if it is a signalling one.
+// Here the result may be any where an operand is NaN: the sums of such a row are NaN.)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
+// Threads that share a row, V vectors of 16 bytes each, in blocks of B; alternatives are chosen among up to kCap logits.
+template <int TPR_, int V_>
+struct Shape {
+    static constexpr int TPR = TPR_, V = V_, B = TPR_ < 256 ? 256 : TPR_, kRows = B / TPR_, kCap = TPR_ < 256 ? 512 : 1024;
+};
+
+// A barrier of the threads that share a row, and their exchange of pairs of values over wavefronts.
+template <typename S>
+struct Group {
+    static constexpr int kWaves = S::TPR / kWave;
+    __device__ static __forceinline__ void sync() {
+        if constexpr (kWaves > 1) __syncthreads();
+        else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+    // f and g over the wavefronts' values; `room` is not written again before the next sync but one
+    template <typename F, typename G>
+    __device__ static __forceinline__ void over_waves(float2* room, float& a, float& b, F f, G g) {
+        if constexpr (kWaves > 1) {
+            if (threadIdx.x % kWave == 0) room[threadIdx.x / kWave] = {a, b};
+            sync();
+            a = room[0].x;
+            b = room[0].y;
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) {
+                a = f(a, room[w].x);
+                b = g(b, room[w].y);
             }
-        }
-        uint64_t before = ~uint64_t{0};
-        for (int k = 0; k < a.top; ++k) {
-            uint64_t best = 0;
-            for (int c = threadIdx.x; c < a.V; c += kThreads) {
-                const float z = load_as_f32(x + c);
-                const uint64_t key = static_cast<uint64_t>(order_of(z)) << 32 | static_cast<uint32_t>(~c);
-                if (z > -INFINITY && key < before && key > best) best = key;
-            }
-            best = over_block(best, [](uint64_t p, uint64_t q) { return p > q ? p : q; });
-            if (threadIdx.x == 0) {
-                const int c = static_cast<int>(~static_cast<uint32_t>(best));
-                a.top_idx[t * a.top + k] = best && log == log ? c : -1;
-                a.top_logp[t * a.top + k] = log != log ? NAN : best ? scaled_difference(load_as_f32(x + c), m0, a.scale) - log : -INFINITY;
-            }
-            before = best;
         }
     }
+    __device__ static __forceinline__ int count(int* room, int v) {
+#pragma unroll
+        for (int o = kWave / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
+        if constexpr (kWaves > 1) {
+            sync();
+            if (threadIdx.x % kWave == 0) room[threadIdx.x / kWave] = v;
+            sync();
+            v = 0;
+            for (int w = 0; w < kWaves; ++w) v += room[w];
+        }
+        return v;
+    }
+};
+
+struct Sums {
+    float m, s, u;  // the largest logit, sum 2^d and sum 2^d d
+};
+
+// What a row's sums and alternatives come to, written by the threads that share the row (`lane` of `threads`).
+struct Row {
+    float m, m0, log;
+    __device__ __forceinline__ Row(const ForwardArgs& a, const Sums& z, int64_t t, float given, bool there, int lane) : m(z.m) {
+        m0 = m == -INFINITY ? 0.f : m;
+        const bool none = z.s == 0.f;
+        log = none ? 0.f : logf(z.s);
+        if (lane == 0) {
+            if (a.rmax) a.rmax[t] = m;
+            if (a.rlog) a.rlog[t] = log;
+            if (a.entropy) a.entropy[t] = none ? 0.f : log - kLn2 * z.u / z.s;
+            if (a.logp) a.logp[t] = there ? scaled_difference(given, m0, a.scale) - log : 0.f;
+        }
+    }
+    // the alternative of rank r (0: none)
+    __device__ __forceinline__ void alternative(const ForwardArgs& a, int64_t t, int r, uint64_t key) const {
+        const float x = logit_of(static_cast<uint32_t>(key >> 32));
+        const bool spoiled = log != log;
+        a.top_idx[t * a.top + r] = key && !spoiled ? static_cast<int32_t>(~static_cast<uint32_t>(key)) : -1;
+        a.top_logp[t * a.top + r] = spoiled ? NAN : key ? scaled_difference(x, m0, a.scale) - log : -INFINITY;
+    }
+};
+
+// The rank of each of `count` keys in LDS among them, by comparing it with all of them: out(rank, key) for ranks below
+// `top`, and out(rank, 0) for those that are left.
+template <typename F>
+__device__ __forceinline__ void rank_keys(const uint64_t* keys, int count, int top, int lane, int threads, F out) {
+    for (int i = lane; i < count; i += threads) {
+        const uint64_t key = keys[i];
+        int r = 0;
+        for (int j = 0; j < count; ++j) r += keys[j] > key;
+        if (r < top) out(r, key);
+    }
+    for (int r = count + lane; r < top; r += threads) out(r, uint64_t{0});
+}
+
+template <typename T, typename S, bool kTop>
+__global__ __launch_bounds__(S::B) void forward_kernel(ForwardArgs a) {
+    constexpr int TPR = S::TPR, V = S::V, N = 16 / sizeof(T);
+    typedef Group<S> G;
+    __shared__ float2 room[2][G::kWaves];
+    __shared__ uint64_t keys[S::kRows][kTop ? S::kCap : 1];
+    __shared__ int found[S::kRows], counts[G::kWaves];
+    const int lane = threadIdx.x % TPR, group = threadIdx.x / TPR;
+    const int64_t items = a.T * a.parts;
+    for (int64_t item = static_cast<int64_t>(blockIdx.x) * S::kRows + group; item < items; item += static_cast<int64_t>(gridDim.x) * S::kRows) {
+        const int64_t t = a.parts == 1 ? item : item / a.parts;
+        const int part = a.parts == 1 ? 0 : static_cast<int>(item - t * a.parts);
+        const auto start = [&](int p) { return p == a.parts ? a.V : static_cast<int>(static_cast<int64_t>(a.V) * p / a.parts) & ~7; };
+        const int first = start(part), len = start(part + 1) - first;
+        const T* row = static_cast<const T*>(a.logits) + t * a.ldl;
+        const T* x0 = row + first;
+        uint32_t target = a.targets.V;
+        float given = 0.f;
+        if (lane == 0) {
+            if (a.logp) target = a.targets[t];
+            if (target < a.targets.V) given = load_as_f32(row + target);
+            found[group] = 0;
+        }
+        // Vector v of this thread: the part's last N logits where fewer are left; those that another vector has, or none, count
+        // as masked.
+        const auto load = [&](int v, Raw<T, N>& x, int& at) {
+            const int c = (v * TPR + lane) * N;
+            at = c + N <= len ? c : len > N ? len - N : 0;
+            if (len >= N) x.load(x0 + at);
+            else x.load_some(x0, len);
+            return c - at;
+        };
+        const auto mask = [&](Raw<T, N>& x, int at, int skip) {
+            if (skip > 0 || len - at < N) {
+                float z[N];
+#pragma unroll
+                for (int i = 0; i < N; ++i) z[i] = i >= skip && at + i < len ? x.get(i) : -INFINITY;
+                x.set(z);
+            }
+        };
+        Raw<T, N> x[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            int at;
+            load(v, x[v], at);
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int c = (v * TPR + lane) * N, at = c + N <= len ? c : len > N ? len - N : 0;
+            mask(x[v], at, c - at);
+        }
+        float m = -INFINITY;
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int i = 0; i < N; i += 2) m = max3(m, x[v].get(i), x[v].get(i + 1));
+        // The least of the maxima of 16, 32 or 64 sets of threads: no alternative is below it.
+        const float own = m;
+        float least;
+        const auto larger = [](float p, float q) { return fmaxf(p, q); };
+        const auto smaller = [](float p, float q) { return fminf(p, q); };
+        const auto plus = [](float p, float q) { return p + q; };
+        {
+            const int set = !kTop ? kWave : a.top > 32 ? TPR / 64 : a.top > 16 ? TPR / 32 : TPR / 16;
+            int o = 1;
+            for (; o < set && o < kWave; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, kWave));
+            least = m;
+            for (; o < kWave; o <<= 1) {
+                m = fmaxf(m, __shfl_xor(m, o, kWave));
+                least = fminf(least, __shfl_xor(least, o, kWave));
+            }
+        }
+        G::over_waves(room[0], m, least, larger, smaller);
+        if constexpr (G::kWaves == 1) G::sync();  // (found is 0 for all)
+        const float m0 = m == -INFINITY ? 0.f : m, c = a.scale * kLog2e, b = -(m0 * c);
+        // 2^(x c + b) is off by a factor of 2^off, the rounding of b, which is known.  Where that is large, or the
+        // product beyond fp32, the difference is formed first.
+        const bool near = fabsf(b) <= 0x1p20f;
+        const float off = near ? fmaf(m0, c, b) : 0.f;
+        float s = 0.f, u = 0.f;
+        const auto sums = [&](auto power) {
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    // (what the pass before made of a logit is not kept: it would take a register for each)
+                    if (i % (4 / sizeof(T)) == 0) asm volatile("" : "+v"(x[v].w[i * sizeof(T) / 4]));
+                    const float d = power(x[v].get(i)), e = __builtin_amdgcn_exp2f(d);
+                    s += e;
+                    u = fmaf(e, fmaxf(d, -200.f), u);  // (0 times minus infinity is 0 here)
+                }
+        };
+        if (near) sums([&](float z) { return fmaf(z, c, b); });
+        else sums([&](float z) { return (z - m0) * c; });
+        // The alternatives, from the row as the cache has it: few threads have one.
+        const auto each = [&](auto f) {
+#pragma unroll 1
+            for (int v = 0; v < V; ++v) {
+                Raw<T, N> y;
+                int at;
+                const int skip = load(v, y, at);
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    if (i >= skip && at + i < len && y.get(i) > -INFINITY) f(y.get(i), first + at + i);
+            }
+        };
+        const auto keep = [&](float z, int token) {
+            const int to = atomicAdd(&found[group], 1);
+            if (to < S::kCap) keys[group][to] = key_of(order_of(z), token);
+        };
+        if (kTop && own >= least && own > -INFINITY)
+            each([&](float z, int token) {
+                if (z >= least) keep(z, token);
+            });
+        s = sum_lanes<kWave>(s);
+        u = sum_lanes<kWave>(u);
+        G::over_waves(room[1], s, u, plus, plus);
+        if constexpr (G::kWaves == 1) G::sync();
+        const float back = __builtin_amdgcn_exp2f(-off);
+        s *= back;
+        const Sums z{m, s, u * back - off * s};
+        int count = kTop ? found[group] : 0;
+        if (kTop && count > S::kCap) {
+            // More logits at the bound and above than there is room for, as where many are alike: the value of the last
+            // alternative, then its token among equals, bit by bit.
+            const auto how_many = [&](auto f) {
+                int n = 0;
+                each([&](float z, int token) { n += f(order_of(z), token); });
+                return G::count(counts, n);
+            };
+            uint32_t value = order_of(least);
+            int above = how_many([&](uint32_t q, int) { return q > value; });
+            if (above >= a.top) {
+                value = 0;
+                for (uint32_t bit = 0x80000000u; bit; bit >>= 1)
+                    if (how_many([&](uint32_t q, int) { return q >= (value | bit); }) >= a.top) value |= bit;
+                above = how_many([&](uint32_t q, int) { return q > value; });
+            }
+            int last = 0;
+            for (int bit = 1 << (31 - __clz(a.V)); bit; bit >>= 1)
+                if (how_many([&](uint32_t q, int j) { return q == value && j < (last | bit); }) < a.top - above) last |= bit;
+            if (lane == 0) found[group] = 0;
+            G::sync();
+            each([&](float z, int token) {
+                const uint32_t q = order_of(z);
+                if (q > value || (q == value && token <= last)) keep(z, token);
+            });
+            G::sync();
+            count = found[group];
+        }
+        if (a.parts == 1) {
+            const Row out(a, z, t, given, target < a.targets.V, lane);
+            if constexpr (kTop) rank_keys(keys[group], count, a.top, lane, TPR, [&](int r, uint64_t key) { out.alternative(a, t, r, key); });
+        } else {
+            if (lane == 0) a.part[item] = {z.m, z.s, z.u, 0.f};
+            if constexpr (kTop)
+                rank_keys(keys[group], count, a.top, lane, TPR, [&](int r, uint64_t key) { a.part_top[item * a.top + r] = key; });
+        }
+        G::sync();  // the next row's threads write what this one's read
+    }
+}
+
+// Rows in parts, one per workgroup at a time.  The parts' alternatives go through LDS as many at a time as there is room for.
+constexpr int kJoin = 256, kJoinKeys = 2048;
+
+template <typename T>
+__global__ __launch_bounds__(kJoin) void join_kernel(ForwardArgs a) {
+    typedef Group<Shape<kJoin, 1>> G;
+    __shared__ float2 room[3][G::kWaves];
+    __shared__ uint64_t keys[kJoinKeys], best[GRASS_LOGP_MOST_TOP];
+    const auto larger = [](float p, float q) { return fmaxf(p, q); };
+    const auto plus = [](float p, float q) { return p + q; };
+    const int lane = threadIdx.x;
+    const float c = a.scale * kLog2e;
+    for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x) {
+        uint32_t target = a.targets.V;
+        float given = 0.f;
+        if (lane == 0) {
+            if (a.logp) target = a.targets[t];
+            if (target < a.targets.V) given = load_as_f32(static_cast<const T*>(a.logits) + t * a.ldl + target);
+        }
+        const float4* part = a.part + t * a.parts;
+        float m = -INFINITY, none = 0.f;
+        for (int p = lane; p < a.parts; p += kJoin) m = fmaxf(m, part[p].x);
+#pragma unroll
+        for (int o = kWave / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, kWave));
+        G::over_waves(room[0], m, none, larger, plus);
+        float s = 0.f, u = 0.f;
+        for (int p = lane; p < a.parts; p += kJoin) {
+            const float4 q = part[p];
+            if (q.y == 0.f) continue;  // all masked
+            const float d = q.x == m ? 0.f : (q.x - m) * c, w = __builtin_amdgcn_exp2f(d);
+            s += w * q.y;
+            if (w > 0.f) u += w * (q.z + d * q.y);
+        }
+        s = sum_lanes<kWave>(s);
+        u = sum_lanes<kWave>(u);
+        G::over_waves(room[1], s, u, plus, plus);
+        const Row out(a, {m, s, u}, t, given, target < a.targets.V, lane);
+        if (a.top) {
+            const uint64_t* from = a.part_top + t * a.parts * a.top;
+            const int64_t all = static_cast<int64_t>(a.parts) * a.top;
+            int kept = 0;
+            for (int64_t at = 0; at < all;) {
+                const int more = static_cast<int>(all - at < kJoinKeys - kept ? all - at : kJoinKeys - kept);
+                for (int i = lane; i < more; i += kJoin) keys[kept + i] = from[at + i];
+                at += more;
+                const int count = kept + more;
+                G::sync();
+                // (those that are none are all alike, and behind the others)
+                for (int i = lane; i < count; i += kJoin) {
+                    const uint64_t key = keys[i];
+                    int r = 0;
+                    for (int j = 0; j < count; ++j) r += keys[j] > key || (keys[j] == key && j < i);
+                    if (r < a.top) best[r] = key;
+                }
+                G::sync();
+                kept = count < a.top ? count : a.top;
+                if (lane < kept) keys[lane] = best[lane];
+            }
+            // (there are `top` of them: every part left as many)
+            if (lane < a.top) out.alternative(a, t, lane, best[lane]);
+        }
+        G::sync();
+    }
+}
+
+// The widest row of one part, and how many parts a row has.
+template <typename T>
+constexpr int kWidest = 16 * 1024 * (16 / sizeof(T));
+template <typename T>
+int parts_of(int64_t T_, int64_t V) {
+    return V <= kWidest<T> ? 1 : static_cast<int>((V + kWidest<T> - 16) / (kWidest<T> - 15));
+}
+
+template <typename T, typename F>
+void by_width(int64_t len, F&& f) {
+    const int64_t vectors = (len * static_cast<int64_t>(sizeof(T)) + 15) / 16;
+    if (vectors <= 64) f(Shape<64, 1>{});
+    else if (vectors <= 128) f(Shape<64, 2>{});
+    else if (vectors <= 256) f(Shape<64, 4>{});
+    else if (vectors <= 512) f(Shape<256, 2>{});
+    else if (vectors <= 1024) f(Shape<256, 4>{});
+    else if (vectors <= 2048) f(Shape<512, 4>{});
+    else if (vectors <= 4096) f(Shape<1024, 4>{});
+    else if (vectors <= 6144) f(Shape<1024, 6>{});
+    else if (vectors <= 8192) f(Shape<1024, 8>{});
+    else if (vectors <= 12288) f(Shape<1024, 12>{});
+    else f(Shape<1024, 16>{});
+}
+
+template <typename T>
+void launch(const ForwardArgs& a, hipStream_t s) {
+    // (parts start on multiples of 8 logits: one has up to 7 more than its share)
+    const int64_t len = a.parts == 1 ? a.V : (a.V + a.parts - 1) / a.parts + 7;
+    by_width<T>(len, [&](auto shape) {
+        typedef decltype(shape) S;
+        const int64_t blocks = (a.T * a.parts + S::kRows - 1) / S::kRows;
+        const unsigned grid = static_cast<unsigned>(blocks < kMostBlocks ? blocks : kMostBlocks);
+        if (a.top) forward_kernel<T, S, true><<<grid, S::B, 0, s>>>(a);
+        else forward_kernel<T, S, false><<<grid, S::B, 0, s>>>(a);
+    });
+    if (a.parts > 1) join_kernel<T><<<static_cast<unsigned>(a.T < kMostBlocks ? a.T : kMostBlocks), kJoin, 0, s>>>(a);
 }
 
 }  // namespace
 
-size_t logp_forward_workspace_bytes(int64_t T, int64_t V, int64_t top, grass_dtype dt) { return 0; }
+size_t logp_forward_workspace_bytes(int64_t T, int64_t V, int64_t top, grass_dtype dt) {
+    const int parts = dt == GRASS_F32 ? parts_of<float>(T, V) : parts_of<uint16_t>(T, V);
+    return parts == 1 ? 0 : static_cast<size_t>(T) * parts * (16 + 8 * top);
+}
 
 grass_status launch_logp_forward(const void* logits, grass_dtype dt, int64_t T, int64_t V, int64_t ldl, const void* targets,
                                  grass_index idt, float scale, float* logp, float* entropy, float* rmax, float* rlog,
                                  int64_t top, float* top_logp, int32_t* top_idx, void* ws, hipStream_t s) {
     if (T == 0) return GRASS_OK;
-    const ForwardArgs a{logits, T, ldl, static_cast<int>(V), static_cast<int>(top), tokens(targets, idt, V), scale,
-                        logp, entropy, rmax, rlog, top_logp, top_idx};
-    const unsigned grid = static_cast<unsigned>(T < kMostBlocks ? T : kMostBlocks);
-    if (dt == GRASS_F32) forward_kernel<float><<<grid, kThreads, 0, s>>>(a);
-    else forward_kernel<uint16_t><<<grid, kThreads, 0, s>>>(a);
+    const int parts = dt == GRASS_F32 ? parts_of<float>(T, V) : parts_of<uint16_t>(T, V);
+    float4* part = static_cast<float4*>(ws);
+    const ForwardArgs a{logits, T, ldl, static_cast<int>(V), static_cast<int>(top), parts, tokens(targets, idt, V), scale,
+                        logp, entropy, rmax, rlog, top_logp, top_idx,
+                        part, parts == 1 ? nullptr : reinterpret_cast<uint64_t*>(part + T * parts)};
+    if (dt == GRASS_F32) launch<float>(a, s);
+    else launch<uint16_t>(a, s);
     return launch_status();
 }
 
