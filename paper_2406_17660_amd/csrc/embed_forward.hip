@@ -2,29 +2,100 @@
 //
 // Bound by memory: Y is written once, and a row of E is read from memory once and from the cache for the other
 // places of its token.
+#include <type_traits>
+
 #include "elem.hpp"
 #include "tokens.hpp"
 
 namespace grass {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kEach = 4;  // vectors of Y a thread has under way
 
-template <typename TE, typename TY>
-__global__ __launch_bounds__(kThreads) void lookup_kernel(const TE* E, int64_t n, int64_t lde, Tokens ids, int64_t T, float scale,
-                                                          TY* Y, int64_t ldy) {
-    for (int64_t t = blockIdx.x; t < T; t += gridDim.x) {
-        const uint32_t v = ids[t];
-        const TE* e = E + v * lde;
-        for (int64_t c = threadIdx.x; c < n; c += kThreads)
-            store_from_f32(Y + t * ldy + c, v < ids.V ? load_as_f32(e + c) * scale : 0.f);
+// u / d for u < 2^31: (u * m) >> shift with m = ceil(2^shift / d), shift = 31 + ceil(log2 d): m d exceeds 2^shift by less than
+// d <= 2^(shift - 31), so that the quotient is off by less than 1 / d.
+struct Divisor {
+    uint32_t d, m;
+    int shift;
+    explicit Divisor(uint32_t by) : d(by) {
+        int s = 0;
+        while ((uint64_t{1} << s) < by) ++s;
+        shift = 31 + s;
+        m = static_cast<uint32_t>(((uint64_t{1} << shift) + by - 1) / by);
+    }
+    __device__ __forceinline__ uint32_t quotient(uint32_t u) const { return static_cast<uint32_t>(static_cast<uint64_t>(u) * m >> shift); }
+};
+
+struct LookupArgs {
+    const void* E;
+    void* Y;
+    int64_t lde, ldy, T;
+    int n;
+    Tokens ids;
+    float scale;
+    Divisor vectors;  // of a row
+};
+
+// Y as one long list of vectors of N values, so that no width leaves threads without work.  A row's last vector is its last N
+// values; what it shares with the one before is written twice, alike.  kCopy: the bits as they are.
+template <typename TE, typename TY, int N, bool kCopy, bool kOnce>
+__global__ __launch_bounds__(kThreads) void lookup_kernel(LookupArgs a) {
+    const uint32_t vectors = a.vectors.d;
+    const int64_t all = a.T * vectors, step = static_cast<int64_t>(gridDim.x) * (kThreads * kEach);
+    for (int64_t start = static_cast<int64_t>(blockIdx.x) * (kThreads * kEach); start < all; start += step) {
+        const int64_t t0 = start / vectors;
+        const uint32_t behind = static_cast<uint32_t>(start - t0 * vectors);
+        Raw<TE, N> e[kEach];
+        TY* y[kEach];
+        bool there[kEach];
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) {
+            const uint32_t place = k * kThreads + threadIdx.x, u = behind + place, q = a.vectors.quotient(u);
+            there[k] = start + place < all;
+            const int64_t t = there[k] ? t0 + q : a.T - 1;
+            const int c = static_cast<int>((u - q * vectors) * N), at = c + N <= a.n ? c : a.n > N ? a.n - N : 0;
+            const uint32_t v = a.ids[t];
+            y[k] = static_cast<TY*>(a.Y) + t * a.ldy + at;
+            const TE* from = static_cast<const TE*>(a.E) + v * a.lde + at;
+            e[k].zero();
+            if (v < a.ids.V && there[k]) {
+                if (a.n >= N) e[k].load(from);
+                else e[k].load_some(from, a.n);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) {
+            if (!there[k]) continue;
+            Raw<TY, N> out;
+            if constexpr (kCopy) {
+#pragma unroll
+                for (int i = 0; i < Raw<TY, N>::kWords; ++i) out.w[i] = e[k].w[i];
+            } else {
+                float z[N];
+#pragma unroll
+                for (int i = 0; i < N; ++i) z[i] = e[k].get(i) * a.scale;
+                out.set(z);
+            }
+            if (a.n >= N) out.template store_as<kOnce>(y[k]);
+            else out.store_some(y[k], a.n);
+        }
     }
 }
 
 template <typename TE, typename TY>
 void launch(const void* E, int64_t n, int64_t lde, const Tokens& ids, int64_t T, float scale, void* Y, int64_t ldy, hipStream_t s) {
-    const unsigned grid = static_cast<unsigned>(T < kMostBlocks ? T : kMostBlocks);
-    lookup_kernel<TE, TY><<<grid, kThreads, 0, s>>>(static_cast<const TE*>(E), n, lde, ids, T, scale, static_cast<TY*>(Y), ldy);
+    constexpr int N = sizeof(TE) == 4 && sizeof(TY) == 4 ? 4 : 8;
+    const LookupArgs a{E, Y, lde, ldy, T, static_cast<int>(n), ids, scale, Divisor(static_cast<uint32_t>((n + N - 1) / N))};
+    const int64_t blocks = (T * a.vectors.d + kThreads * kEach - 1) / (kThreads * kEach);
+    const unsigned grid = static_cast<unsigned>(blocks < kMostBlocks ? blocks : kMostBlocks);
+    const bool once = static_cast<double>(T) * n * sizeof(TY) > kStreamed;
+    const auto go = [&](auto copy) {
+        constexpr bool kCopy = decltype(copy)::value;
+        once ? lookup_kernel<TE, TY, N, kCopy, true><<<grid, kThreads, 0, s>>>(a) : lookup_kernel<TE, TY, N, kCopy, false><<<grid, kThreads, 0, s>>>(a);
+    };
+    if constexpr (std::is_same<TE, TY>::value)
+        if (scale == 1.f) return go(std::true_type{});
+    go(std::false_type{});
 }
 
 }  // namespace
