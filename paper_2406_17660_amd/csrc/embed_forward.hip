@@ -53,7 +53,7 @@ __global__ __launch_bounds__(kThreads) void lookup_kernel(LookupArgs a) {
             const uint32_t place = k * kThreads + threadIdx.x, u = behind + place, q = a.vectors.quotient(u);
             there[k] = start + place < all;
             const int64_t t = there[k] ? t0 + q : a.T - 1;
-            const int c = static_cast<int>((u - q * vectors) * N), at = c + N <= a.n ? c : a.n > N ? a.n - N : 0;
+            const int64_t c = static_cast<int64_t>(u - q * vectors) * N, at = c + N <= a.n ? c : a.n > N ? a.n - N : 0;
             const uint32_t v = a.ids[t];
             y[k] = static_cast<TY*>(a.Y) + t * a.ldy + at;
             const TE* from = static_cast<const TE*>(a.E) + v * a.lde + at;

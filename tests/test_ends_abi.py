@@ -40,7 +40,7 @@ def embed_backward(**kw):
     (SHAPE, dict(V=0)), (SHAPE, dict(V=BIG)), (SHAPE, dict(n=0)), (SHAPE, dict(n=BIG)), (SHAPE, dict(lddy=63)), (SHAPE, dict(ldde=63)),
     (SHAPE, dict(scale=NAN)), (SHAPE, dict(scale=-INF)), (SHAPE, dict(dY=ODD)), (SHAPE, dict(dE=FAKE + 2)), (SHAPE, dict(ids=FAKE + 4)),
     (DTYPE, dict(dt=2)), (DTYPE, dict(gdt=7)), (DTYPE, dict(idt=-1)), (OK, dict(T=0, accumulate=1)),
-    (OK, dict(T=0, accumulate=1, dY=None, ids=None, ws=None, ws_bytes=0))])
+    (OK, dict(T=0, accumulate=1, dY=None, ids=None))])
 def test_embed_backward_validation(want, kw):
     assert embed_backward(**kw) == want
 
