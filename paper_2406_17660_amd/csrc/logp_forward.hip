@@ -3,6 +3,8 @@
 // Bound by memory: a row is read once and stays in the registers of the threads that share it, for its maximum, its
 // sums and its alternatives.  With c = scale log2(e) and d = (x - rmax) c, s = sum 2^d and u = sum 2^d d give
 // rlog = ln s and entropy = ln s - ln(2) u / s.
+#include <type_traits>
+
 #include "elem.hpp"
 #include "tokens.hpp"
 
@@ -88,6 +90,28 @@ struct Group {
     }
 };
 
+// f of a lane's value and of another's 2^kStep lanes away, where lanes that were together in the steps before have the same value.
+template <int kStep, typename F>
+__device__ __forceinline__ float fold(float v, F f) {
+    if constexpr (kStep < 4) {
+        constexpr int kCtrl = kStep == 0 ? 0xB1 : kStep == 1 ? 0x4E : kStep == 2 ? 0x141 : 0x140;  // (as in sum_lanes)
+        return f(v, dpp<kCtrl>(v));
+    } else {
+        const uint32_t a = __float_as_uint(v);
+        const auto r = kStep == 4 ? __builtin_amdgcn_permlane16_swap(a, a, false, false) : __builtin_amdgcn_permlane32_swap(a, a, false, false);
+        return f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+}
+template <typename F>
+__device__ __forceinline__ void over_lanes(F step) {
+    step(std::integral_constant<int, 0>{});
+    step(std::integral_constant<int, 1>{});
+    step(std::integral_constant<int, 2>{});
+    step(std::integral_constant<int, 3>{});
+    step(std::integral_constant<int, 4>{});
+    step(std::integral_constant<int, 5>{});
+}
+
 struct Sums {
     float m, s, u;  // the largest logit, sum 2^d and sum 2^d d
 };
@@ -116,69 +140,101 @@ struct Row {
 };
 
 // The rank of each of `count` keys in LDS among them, by comparing it with all of them: out(rank, key) for ranks below
-// `top`, and out(rank, 0) for those that are left.
-template <typename F>
-__device__ __forceinline__ void rank_keys(const uint64_t* keys, int count, int top, int lane, int threads, F out) {
-    for (int i = lane; i < count; i += threads) {
+// `top`, and out(rank, 0) for those that are left.  Where there are fewer keys than threads, several compare for each; ranks:
+// room for as many as there are keys, zeros, and zeros again afterwards (sync() between its uses).
+template <typename Sync, typename F>
+__device__ __forceinline__ void rank_keys(const uint64_t* keys, int* ranks, int count, int top, int lane, int threads, Sync sync, F out) {
+    int each = 1;
+    while (2 * each * count <= threads && each < 16) each *= 2;
+    for (int i = lane / each; i < count; i += threads / each) {
         const uint64_t key = keys[i];
         int r = 0;
-        for (int j = 0; j < count; ++j) r += keys[j] > key;
-        if (r < top) out(r, key);
+#pragma unroll 4
+        for (int j = lane % each; j < count; j += each) r += keys[j] > key;
+        if (each == 1) ranks[i] = r;
+        else if (r) atomicAdd(&ranks[i], r);
+    }
+    sync();
+    for (int i = lane; i < count; i += threads) {
+        const int r = ranks[i];
+        ranks[i] = 0;
+        if (r < top) out(r, keys[i]);
     }
     for (int r = count + lane; r < top; r += threads) out(r, uint64_t{0});
 }
 
-template <typename T, typename S, bool kTop>
-__global__ __launch_bounds__(S::B) void forward_kernel(ForwardArgs a) {
-    constexpr int TPR = S::TPR, V = S::V, N = 16 / sizeof(T);
-    typedef Group<S> G;
-    __shared__ float2 room[2][G::kWaves];
-    __shared__ uint64_t keys[S::kRows][kTop ? S::kCap : 1];
-    __shared__ int found[S::kRows], counts[G::kWaves];
-    const int lane = threadIdx.x % TPR, group = threadIdx.x / TPR;
-    const int64_t items = a.T * a.parts;
-    for (int64_t item = static_cast<int64_t>(blockIdx.x) * S::kRows + group; item < items; item += static_cast<int64_t>(gridDim.x) * S::kRows) {
-        const int64_t t = a.parts == 1 ? item : item / a.parts;
+// A row, or a part of one: where it starts, how many logits it has, and the token of the first.
+template <typename T, typename S>
+struct Piece {
+    static constexpr int N = 16 / sizeof(T);
+    int64_t item, t;
+    int first, len;
+    const T* x0;
+    __device__ __forceinline__ Piece(const ForwardArgs& a, int64_t at) : item(at) {
+        t = a.parts == 1 ? item : item / a.parts;
         const int part = a.parts == 1 ? 0 : static_cast<int>(item - t * a.parts);
         const auto start = [&](int p) { return p == a.parts ? a.V : static_cast<int>(static_cast<int64_t>(a.V) * p / a.parts) & ~7; };
-        const int first = start(part), len = start(part + 1) - first;
-        const T* row = static_cast<const T*>(a.logits) + t * a.ldl;
-        const T* x0 = row + first;
+        first = start(part);
+        len = start(part + 1) - first;
+        x0 = static_cast<const T*>(a.logits) + t * a.ldl + first;
+    }
+    // Where vector v of a thread starts: at the last N logits where fewer are left.  Those that another vector has, or
+    // none, count as masked.
+    __device__ __forceinline__ int at(int v, int lane) const {
+        const int c = (v * S::TPR + lane) * N;
+        return c + N <= len ? c : len > N ? len - N : 0;
+    }
+    template <bool kOnce>
+    __device__ __forceinline__ void load(int v, int lane, Raw<T, N>& x) const {
+        if (len >= N) x.template load_as<kOnce>(x0 + at(v, lane));
+        else x.load_some(x0, len);
+    }
+    __device__ __forceinline__ void mask(int v, int lane, Raw<T, N>& x) const {
+        const int c = (v * S::TPR + lane) * N, from = at(v, lane);
+        if (c > from || len < N) {
+            float z[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) z[i] = from + i >= c && from + i < len ? x.get(i) : -INFINITY;
+            x.set(z);
+        }
+    }
+};
+
+template <typename T, typename S, bool kTop, bool kEntropy, bool kOnce>
+__global__ __launch_bounds__(S::B) __attribute__((amdgpu_waves_per_eu(8))) void forward_kernel(ForwardArgs a) {
+    constexpr int TPR = S::TPR, V = S::V, N = 16 / sizeof(T);
+    typedef Group<S> G;
+    typedef Raw<T, N> Vector;
+    __shared__ float2 room[2][G::kWaves];
+    __shared__ uint64_t keys[S::kRows][kTop ? S::kCap : 1];
+    __shared__ int found[S::kRows], counts[G::kWaves], ranks[S::kRows][kTop ? S::kCap : 1];
+    const int lane = threadIdx.x % TPR, group = S::kRows == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
+    // `lane` again, so that what an earlier step made of it is not kept: each thread has the registers of eight wavefronts to a SIMD.
+    const auto lane_again = [&] {
+        int l = lane;
+        asm volatile("" : "+v"(l));
+        return l;
+    };
+    if constexpr (kTop) {
+        for (int i = lane; i < S::kCap; i += TPR) ranks[group][i] = 0;
+        G::sync();
+    }
+    const auto work = [&](int64_t item) {
+        const Piece<T, S> row(a, item);
+        const int64_t t = row.t;
+        Vector x[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) row.template load<kOnce>(v, lane, x[v]);
         uint32_t target = a.targets.V;
         float given = 0.f;
         if (lane == 0) {
-            if (a.logp) target = a.targets[t];
-            if (target < a.targets.V) given = load_as_f32(row + target);
+            if (a.logp && a.parts == 1) target = a.targets[t];
+            if (target < a.targets.V) given = load_as_f32(row.x0 + target);
             found[group] = 0;
         }
-        // Vector v of this thread: the part's last N logits where fewer are left; those that another vector has, or none, count
-        // as masked.
-        const auto load = [&](int v, Raw<T, N>& x, int& at) {
-            const int c = (v * TPR + lane) * N;
-            at = c + N <= len ? c : len > N ? len - N : 0;
-            if (len >= N) x.load(x0 + at);
-            else x.load_some(x0, len);
-            return c - at;
-        };
-        const auto mask = [&](Raw<T, N>& x, int at, int skip) {
-            if (skip > 0 || len - at < N) {
-                float z[N];
+        const int masking = lane_again();
 #pragma unroll
-                for (int i = 0; i < N; ++i) z[i] = i >= skip && at + i < len ? x.get(i) : -INFINITY;
-                x.set(z);
-            }
-        };
-        Raw<T, N> x[V];
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            int at;
-            load(v, x[v], at);
-        }
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int c = (v * TPR + lane) * N, at = c + N <= len ? c : len > N ? len - N : 0;
-            mask(x[v], at, c - at);
-        }
+        for (int v = 0; v < V; ++v) row.mask(v, masking, x[v]);
         float m = -INFINITY;
 #pragma unroll
         for (int v = 0; v < V; ++v)
@@ -190,16 +246,13 @@ __global__ __launch_bounds__(S::B) void forward_kernel(ForwardArgs a) {
         const auto larger = [](float p, float q) { return fmaxf(p, q); };
         const auto smaller = [](float p, float q) { return fminf(p, q); };
         const auto plus = [](float p, float q) { return p + q; };
-        {
-            const int set = !kTop ? kWave : a.top > 32 ? TPR / 64 : a.top > 16 ? TPR / 32 : TPR / 16;
-            int o = 1;
-            for (; o < set && o < kWave; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, kWave));
-            least = m;
-            for (; o < kWave; o <<= 1) {
-                m = fmaxf(m, __shfl_xor(m, o, kWave));
-                least = fminf(least, __shfl_xor(least, o, kWave));
-            }
-        }
+        least = m;
+        const int set = a.top > 32 ? TPR / 64 : a.top > 16 ? TPR / 32 : TPR / 16;
+        over_lanes([&](auto step) {
+            constexpr int kStep = decltype(step)::value;
+            m = fold<kStep>(m, larger);
+            if constexpr (kTop) least = (1 << kStep) < set ? m : fold<kStep>(least, smaller);
+        });
         G::over_waves(room[0], m, least, larger, smaller);
         if constexpr (G::kWaves == 1) G::sync();  // (found is 0 for all)
         const float m0 = m == -INFINITY ? 0.f : m, c = a.scale * kLog2e, b = -(m0 * c);
@@ -217,33 +270,39 @@ __global__ __launch_bounds__(S::B) void forward_kernel(ForwardArgs a) {
                     if (i % (4 / sizeof(T)) == 0) asm volatile("" : "+v"(x[v].w[i * sizeof(T) / 4]));
                     const float d = power(x[v].get(i)), e = __builtin_amdgcn_exp2f(d);
                     s += e;
-                    u = fmaf(e, fmaxf(d, -200.f), u);  // (0 times minus infinity is 0 here)
+                    if constexpr (kEntropy) u = fmaf(e, fmaxf(d, -200.f), u);  // (0 times minus infinity is 0 here)
                 }
         };
-        if (near) sums([&](float z) { return fmaf(z, c, b); });
-        else sums([&](float z) { return (z - m0) * c; });
-        // The alternatives, from the row as the cache has it: few threads have one.
-        const auto each = [&](auto f) {
-#pragma unroll 1
-            for (int v = 0; v < V; ++v) {
-                Raw<T, N> y;
-                int at;
-                const int skip = load(v, y, at);
-#pragma unroll
-                for (int i = 0; i < N; ++i)
-                    if (i >= skip && at + i < len && y.get(i) > -INFINITY) f(y.get(i), first + at + i);
-            }
-        };
+        if constexpr (kTop) {  // (one loop: what is left of the registers goes to the alternatives)
+            const float z0 = near ? 0.f : m0, b0 = near ? b : 0.f;
+            sums([&](float z) { return fmaf(z - z0, c, b0); });
+            asm volatile("" : "+v"(s), "+v"(u));  // (and not behind them)
+        } else {
+            if (near) sums([&](float z) { return fmaf(z, c, b); });
+            else sums([&](float z) { return (z - m0) * c; });
+        }
         const auto keep = [&](float z, int token) {
             const int to = atomicAdd(&found[group], 1);
             if (to < S::kCap) keys[group][to] = key_of(order_of(z), token);
         };
-        if (kTop && own >= least && own > -INFINITY)
-            each([&](float z, int token) {
-                if (z >= least) keep(z, token);
-            });
+        if (kTop && own >= least && own > -INFINITY) {  // (few threads)
+            const int place = lane_again();
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+#pragma unroll
+                for (int k = 0; k < Vector::kWords; ++k) asm volatile("" : "+v"(x[v].w[k]));
+                float best = -INFINITY;
+#pragma unroll
+                for (int i = 0; i < N; i += 2) best = max3(best, x[v].get(i), x[v].get(i + 1));
+                if (best < least) continue;
+                const int token = row.first + row.at(v, place);
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    if (x[v].get(i) >= least && x[v].get(i) > -INFINITY) keep(x[v].get(i), token + i);
+            }
+        }
         s = sum_lanes<kWave>(s);
-        u = sum_lanes<kWave>(u);
+        if constexpr (kEntropy) u = sum_lanes<kWave>(u);
         G::over_waves(room[1], s, u, plus, plus);
         if constexpr (G::kWaves == 1) G::sync();
         const float back = __builtin_amdgcn_exp2f(-off);
@@ -253,6 +312,19 @@ __global__ __launch_bounds__(S::B) void forward_kernel(ForwardArgs a) {
         if (kTop && count > S::kCap) {
             // More logits at the bound and above than there is room for, as where many are alike: the value of the last
             // alternative, then its token among equals, bit by bit.
+            // (Read again: with the row's registers in these loops others would not do.)
+            const int place = lane_again();
+            const auto each = [&](auto f) {
+#pragma unroll 1
+                for (int v = 0; v < V; ++v) {
+                    Vector y;
+                    row.template load<false>(v, place, y);
+                    row.mask(v, place, y);
+#pragma unroll
+                    for (int i = 0; i < N; ++i)
+                        if (y.get(i) > -INFINITY) f(y.get(i), row.first + row.at(v, place) + i);
+                }
+            };
             const auto how_many = [&](auto f) {
                 int n = 0;
                 each([&](float z, int token) { n += f(order_of(z), token); });
@@ -280,14 +352,18 @@ __global__ __launch_bounds__(S::B) void forward_kernel(ForwardArgs a) {
         }
         if (a.parts == 1) {
             const Row out(a, z, t, given, target < a.targets.V, lane);
-            if constexpr (kTop) rank_keys(keys[group], count, a.top, lane, TPR, [&](int r, uint64_t key) { out.alternative(a, t, r, key); });
+            if constexpr (kTop)
+                rank_keys(keys[group], ranks[group], count, a.top, lane, TPR, G::sync, [&](int r, uint64_t key) { out.alternative(a, t, r, key); });
         } else {
             if (lane == 0) a.part[item] = {z.m, z.s, z.u, 0.f};
             if constexpr (kTop)
-                rank_keys(keys[group], count, a.top, lane, TPR, [&](int r, uint64_t key) { a.part_top[item * a.top + r] = key; });
+                rank_keys(keys[group], ranks[group], count, a.top, lane, TPR, G::sync,
+                          [&](int r, uint64_t key) { a.part_top[item * a.top + r] = key; });
         }
         G::sync();  // the next row's threads write what this one's read
-    }
+    };
+    const int64_t items = a.T * a.parts, step = static_cast<int64_t>(gridDim.x) * S::kRows;
+    for (int64_t item = static_cast<int64_t>(blockIdx.x) * S::kRows + group; item < items; item += step) work(item);
 }
 
 // Rows in parts, one per workgroup at a time.  The parts' alternatives go through LDS as many at a time as there is room for.
@@ -357,10 +433,11 @@ __global__ __launch_bounds__(kJoin) void join_kernel(ForwardArgs a) {
 
 // The widest row of one part, and how many parts a row has.
 template <typename T>
-constexpr int kWidest = 16 * 1024 * (16 / sizeof(T));
+constexpr int kWidest = 8 * 1024 * (16 / sizeof(T));
 template <typename T>
-int parts_of(int64_t T_, int64_t V) {
-    return V <= kWidest<T> ? 1 : static_cast<int>((V + kWidest<T> - 16) / (kWidest<T> - 15));
+int parts_of(int64_t rows, int64_t V) {
+    const int64_t least = V <= kWidest<T> ? 1 : (V + kWidest<T> - 16) / (kWidest<T> - 15);
+    return static_cast<int>(least);
 }
 
 template <typename T, typename F>
@@ -369,14 +446,14 @@ void by_width(int64_t len, F&& f) {
     if (vectors <= 64) f(Shape<64, 1>{});
     else if (vectors <= 128) f(Shape<64, 2>{});
     else if (vectors <= 256) f(Shape<64, 4>{});
-    else if (vectors <= 512) f(Shape<256, 2>{});
+    else if (vectors <= 512) f(Shape<64, 8>{});
     else if (vectors <= 1024) f(Shape<256, 4>{});
-    else if (vectors <= 2048) f(Shape<512, 4>{});
-    else if (vectors <= 4096) f(Shape<1024, 4>{});
+    else if (vectors <= 2048) f(Shape<256, 8>{});
+    else if (vectors <= 2560) f(Shape<512, 5>{});
+    else if (vectors <= 4096) f(Shape<512, 8>{});
     else if (vectors <= 6144) f(Shape<1024, 6>{});
-    else if (vectors <= 8192) f(Shape<1024, 8>{});
-    else if (vectors <= 12288) f(Shape<1024, 12>{});
-    else f(Shape<1024, 16>{});
+    else if (vectors <= 7168) f(Shape<1024, 7>{});
+    else f(Shape<1024, 8>{});
 }
 
 template <typename T>
@@ -387,8 +464,13 @@ void launch(const ForwardArgs& a, hipStream_t s) {
         typedef decltype(shape) S;
         const int64_t blocks = (a.T * a.parts + S::kRows - 1) / S::kRows;
         const unsigned grid = static_cast<unsigned>(blocks < kMostBlocks ? blocks : kMostBlocks);
-        if (a.top) forward_kernel<T, S, true><<<grid, S::B, 0, s>>>(a);
-        else forward_kernel<T, S, false><<<grid, S::B, 0, s>>>(a);
+        const bool once = static_cast<double>(a.T) * a.V * sizeof(T) > kStreamed;
+        const auto go = [&](auto top, auto entropy, auto stream) {
+            forward_kernel<T, S, decltype(top)::value, decltype(entropy)::value, decltype(stream)::value><<<grid, S::B, 0, s>>>(a);
+        };
+        const auto with_entropy = [&](auto top, auto entropy) { once ? go(top, entropy, std::true_type{}) : go(top, entropy, std::false_type{}); };
+        const auto with_top = [&](auto top) { a.entropy ? with_entropy(top, std::true_type{}) : with_entropy(top, std::false_type{}); };
+        a.top ? with_top(std::true_type{}) : with_top(std::false_type{});
     });
     if (a.parts > 1) join_kernel<T><<<static_cast<unsigned>(a.T < kMostBlocks ? a.T : kMostBlocks), kJoin, 0, s>>>(a);
 }
