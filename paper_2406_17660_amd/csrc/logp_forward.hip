@@ -31,6 +31,7 @@ __device__ __forceinline__ uint32_t order_of(float x) {
     const uint32_t u = __float_as_uint(x + 0.f);
     return (u >> 31) ? ~u : u | 0x80000000u;
 }
+constexpr uint32_t kMasked = 0x007FFFFFu;  // of minus infinity
 __device__ __forceinline__ float logit_of(uint32_t order) {
     return __uint_as_float((order >> 31) ? order & 0x7FFFFFFFu : ~order);
 }
@@ -207,8 +208,10 @@ __global__ __launch_bounds__(S::B) __attribute__((amdgpu_waves_per_eu(8))) void 
     typedef Raw<T, N> Vector;
     __shared__ float2 room[2][G::kWaves];
     __shared__ uint64_t keys[S::kRows][kTop ? S::kCap : 1];
+    __shared__ float sets[kWave];
     __shared__ int found[S::kRows], counts[G::kWaves], ranks[S::kRows][kTop ? S::kCap : 1];
-    const int lane = threadIdx.x % TPR, group = S::kRows == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
+    const int lane = threadIdx.x % TPR, wave0 = __builtin_amdgcn_readfirstlane(lane);
+    const int group = S::kRows == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
     // `lane` again, so that what an earlier step made of it is not kept: each thread has the registers of eight wavefronts to a SIMD.
     const auto lane_again = [&] {
         int l = lane;
@@ -223,8 +226,11 @@ __global__ __launch_bounds__(S::B) __attribute__((amdgpu_waves_per_eu(8))) void 
         const Piece<T, S> row(a, item);
         const int64_t t = row.t;
         Vector x[V];
+        // Whether the wavefront has logits of vector v at all.
+        const auto some = [&](int v) { return (v * TPR + wave0) * N < row.len; };
 #pragma unroll
-        for (int v = 0; v < V; ++v) row.template load<kOnce>(v, lane, x[v]);
+        for (int v = 0; v < V; ++v)
+            if (some(v)) row.template load<kOnce>(v, lane, x[v]);
         uint32_t target = a.targets.V;
         float given = 0.f;
         if (lane == 0) {
@@ -234,27 +240,46 @@ __global__ __launch_bounds__(S::B) __attribute__((amdgpu_waves_per_eu(8))) void 
         }
         const int masking = lane_again();
 #pragma unroll
-        for (int v = 0; v < V; ++v) row.mask(v, masking, x[v]);
+        for (int v = 0; v < V; ++v)
+            if (some(v)) row.mask(v, masking, x[v]);
         float m = -INFINITY;
 #pragma unroll
         for (int v = 0; v < V; ++v)
+            if (some(v))
 #pragma unroll
-            for (int i = 0; i < N; i += 2) m = max3(m, x[v].get(i), x[v].get(i + 1));
-        // The least of the maxima of 16, 32 or 64 sets of threads: no alternative is below it.
+                for (int i = 0; i < N; i += 2) m = max3(m, x[v].get(i), x[v].get(i + 1));
         const float own = m;
-        float least;
+        float least = -INFINITY;
         const auto larger = [](float p, float q) { return fmaxf(p, q); };
-        const auto smaller = [](float p, float q) { return fminf(p, q); };
         const auto plus = [](float p, float q) { return p + q; };
-        least = m;
-        const int set = a.top > 32 ? TPR / 64 : a.top > 16 ? TPR / 32 : TPR / 16;
-        over_lanes([&](auto step) {
-            constexpr int kStep = decltype(step)::value;
-            m = fold<kStep>(m, larger);
-            if constexpr (kTop) least = (1 << kStep) < set ? m : fold<kStep>(least, smaller);
-        });
-        G::over_waves(room[0], m, least, larger, smaller);
-        if constexpr (G::kWaves == 1) G::sync();  // (found is 0 for all)
+        if constexpr (kTop) {
+            // The threads in 64 sets: as many as `top` of these have a logit not below the `top`-th largest of their maxima, so that
+            // no alternative is below it, and few other logits are above.  It is found bit by bit (down to some, which is low enough).
+            constexpr int kSet = TPR / kWave, kBits = sizeof(T) == 2 ? 16 : 20;
+            over_lanes([&](auto step) {
+                constexpr int kStep = decltype(step)::value;
+                if constexpr ((1 << kStep) < kSet) m = fold<kStep>(m, larger);
+            });
+            if constexpr (kSet > 1) {
+                if (lane % kSet == 0) sets[lane / kSet] = m;
+                G::sync();
+                m = sets[threadIdx.x % kWave];
+            }
+            const uint32_t order = order_of(m);
+            uint32_t bound = 0;
+            for (uint32_t bit = 0x80000000u; bit >> (32 - kBits); bit >>= 1) {
+                const int n = __popcll(__ballot(order >= (bound | bit)));
+                if (n >= a.top) bound |= bit;
+                if (n == a.top) break;
+            }
+            if (bound > kMasked) least = logit_of(bound);
+            over_lanes([&](auto step) { m = fold<decltype(step)::value>(m, larger); });
+            if constexpr (kSet == 1) G::sync();  // (found is 0 for all)
+        } else {
+            float none = 0.f;
+            over_lanes([&](auto step) { m = fold<decltype(step)::value>(m, larger); });
+            G::over_waves(room[0], m, none, larger, plus);
+        }
         const float m0 = m == -INFINITY ? 0.f : m, c = a.scale * kLog2e, b = -(m0 * c);
         // 2^(x c + b) is off by a factor of 2^off, the rounding of b, which is known.  Where that is large, or the
         // product beyond fp32, the difference is formed first.
@@ -263,7 +288,8 @@ __global__ __launch_bounds__(S::B) __attribute__((amdgpu_waves_per_eu(8))) void 
         float s = 0.f, u = 0.f;
         const auto sums = [&](auto power) {
 #pragma unroll
-            for (int v = 0; v < V; ++v)
+            for (int v = 0; v < V; ++v) {
+                if (!some(v)) continue;
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
                     // (what the pass before made of a logit is not kept: it would take a register for each)
@@ -272,6 +298,7 @@ __global__ __launch_bounds__(S::B) __attribute__((amdgpu_waves_per_eu(8))) void 
                     s += e;
                     if constexpr (kEntropy) u = fmaf(e, fmaxf(d, -200.f), u);  // (0 times minus infinity is 0 here)
                 }
+            }
         };
         if constexpr (kTop) {  // (one loop: what is left of the registers goes to the alternatives)
             const float z0 = near ? 0.f : m0, b0 = near ? b : 0.f;
@@ -289,6 +316,7 @@ __global__ __launch_bounds__(S::B) __attribute__((amdgpu_waves_per_eu(8))) void 
             const int place = lane_again();
 #pragma unroll
             for (int v = 0; v < V; ++v) {
+                if (!some(v)) continue;
 #pragma unroll
                 for (int k = 0; k < Vector::kWords; ++k) asm volatile("" : "+v"(x[v].w[k]));
                 float best = -INFINITY;
@@ -373,7 +401,9 @@ template <typename T>
 __global__ __launch_bounds__(kJoin) void join_kernel(ForwardArgs a) {
     typedef Group<Shape<kJoin, 1>> G;
     __shared__ float2 room[3][G::kWaves];
-    __shared__ uint64_t keys[kJoinKeys], best[GRASS_LOGP_MOST_TOP];
+    __shared__ uint64_t keys[kJoinKeys], best[GRASS_LOGP_MOST_TOP], bounds[G::kWaves];
+    __shared__ int ranks[kJoinKeys], found;
+    for (int i = threadIdx.x; i < kJoinKeys; i += kJoin) ranks[i] = 0;
     const auto larger = [](float p, float q) { return fmaxf(p, q); };
     const auto plus = [](float p, float q) { return p + q; };
     const int lane = threadIdx.x;
@@ -406,26 +436,37 @@ __global__ __launch_bounds__(kJoin) void join_kernel(ForwardArgs a) {
         if (a.top) {
             const uint64_t* from = a.part_top + t * a.parts * a.top;
             const int64_t all = static_cast<int64_t>(a.parts) * a.top;
-            int kept = 0;
-            for (int64_t at = 0; at < all;) {
-                const int more = static_cast<int>(all - at < kJoinKeys - kept ? all - at : kJoinKeys - kept);
-                for (int i = lane; i < more; i += kJoin) keys[kept + i] = from[at + i];
-                at += more;
-                const int count = kept + more;
-                G::sync();
-                // (those that are none are all alike, and behind the others)
-                for (int i = lane; i < count; i += kJoin) {
-                    const uint64_t key = keys[i];
-                    int r = 0;
-                    for (int j = 0; j < count; ++j) r += keys[j] > key || (keys[j] == key && j < i);
-                    if (r < a.top) best[r] = key;
+            // no alternative is behind the last one of any part that has as many
+            uint64_t bound = 1;
+            for (int p = lane; p < a.parts; p += kJoin) {
+                const uint64_t last = from[static_cast<int64_t>(p + 1) * a.top - 1];
+                bound = last > bound ? last : bound;
+            }
+#pragma unroll
+            for (int o = kWave / 2; o > 0; o >>= 1) {
+                const uint64_t other = __shfl_xor(bound, o, kWave);
+                bound = other > bound ? other : bound;
+            }
+            if (lane % kWave == 0) bounds[lane / kWave] = bound;
+            if (lane == 0) found = 0;
+            G::sync();
+            for (int w = 0; w < G::kWaves; ++w) bound = bounds[w] > bound ? bounds[w] : bound;
+            for (int64_t at = 0; at < all; at += kJoin) {
+                if (at + lane < all) {
+                    const uint64_t key = from[at + lane];
+                    if (key >= bound) keys[atomicAdd(&found, 1)] = key;
                 }
                 G::sync();
-                kept = count < a.top ? count : a.top;
-                if (lane < kept) keys[lane] = best[lane];
+                const int count = found;
+                if (count > kJoinKeys - kJoin && at + kJoin < all) {  // no room for as many again: the best of them
+                    rank_keys(keys, ranks, count, a.top, lane, kJoin, G::sync, [&](int r, uint64_t key) { best[r] = key; });
+                    G::sync();
+                    if (lane < a.top) keys[lane] = best[lane];
+                    if (lane == 0) found = a.top;
+                }
+                G::sync();
             }
-            // (there are `top` of them: every part left as many)
-            if (lane < a.top) out.alternative(a, t, lane, best[lane]);
+            rank_keys(keys, ranks, found, a.top, lane, kJoin, G::sync, [&](int r, uint64_t key) { out.alternative(a, t, r, key); });
         }
         G::sync();
     }
@@ -433,7 +474,7 @@ __global__ __launch_bounds__(kJoin) void join_kernel(ForwardArgs a) {
 
 // The widest row of one part, and how many parts a row has.
 template <typename T>
-constexpr int kWidest = 8 * 1024 * (16 / sizeof(T));
+constexpr int kWidest = 8 * 512 * (16 / sizeof(T));
 template <typename T>
 int parts_of(int64_t rows, int64_t V) {
     const int64_t least = V <= kWidest<T> ? 1 : (V + kWidest<T> - 16) / (kWidest<T> - 15);
@@ -450,10 +491,7 @@ void by_width(int64_t len, F&& f) {
     else if (vectors <= 1024) f(Shape<256, 4>{});
     else if (vectors <= 2048) f(Shape<256, 8>{});
     else if (vectors <= 2560) f(Shape<512, 5>{});
-    else if (vectors <= 4096) f(Shape<512, 8>{});
-    else if (vectors <= 6144) f(Shape<1024, 6>{});
-    else if (vectors <= 7168) f(Shape<1024, 7>{});
-    else f(Shape<1024, 8>{});
+    else f(Shape<512, 8>{});
 }
 
 template <typename T>
