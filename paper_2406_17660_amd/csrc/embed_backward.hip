@@ -28,7 +28,7 @@ struct SortArgs {
     int shift, bits, blocks;
     uint32_t* counts;   // blocks x 2^bits
     uint8_t* present;   // NULL, or a byte for each token: whether it occurs
-    uint32_t* longs;    // how many tokens have more than kPiece places: 0 here
+    uint32_t* found;    // how many tokens have more places than a piece: 0 here; and how many places are listed
 };
 
 __device__ __forceinline__ Place place_at(const SortArgs& a, int64_t i) {
@@ -46,45 +46,127 @@ __device__ __forceinline__ uint64_t same_digit(uint32_t digit, int bits, bool th
     return same;
 }
 
-// f(i, place, digit, lanes of the same digit) for 64 places at a time of the wavefront's share of the workgroup's chunk.
-template <typename F>
-__device__ __forceinline__ void each_place(const SortArgs& a, F f) {
-    const int64_t share = a.chunk / kSortWaves, start = blockIdx.x * a.chunk + threadIdx.x / kWave * share;
-    for (int64_t at = start; at < start + share && at < a.T; at += kWave) {
-        const int64_t i = at + threadIdx.x % kWave;
-        const bool there = i < a.T;
-        const Place p = there ? place_at(a, i) : Place{0, 0};
-        const uint32_t digit = p.token >> a.shift & ((1u << a.bits) - 1);
-        f(p, digit, same_digit(digit, a.bits, there), there);
-    }
+// 64 places of a wavefront at a time: what each lane has, and which of them have its digit.
+struct Step {
+    Place p;
+    uint32_t digit;
+    uint64_t same;
+    bool there;
+    __device__ __forceinline__ bool leads() const { return there && (same & ((uint64_t{1} << threadIdx.x % kWave) - 1)) == 0; }
+    __device__ __forceinline__ int before() const { return __popcll(same & ((uint64_t{1} << threadIdx.x % kWave) - 1)); }
+};
+__device__ __forceinline__ Step step_of(Place p, bool there, int shift, int bits) {
+    Step s;
+    s.p = p;
+    s.there = there;
+    s.digit = p.token >> shift & ((1u << bits) - 1);
+    s.same = same_digit(s.digit, bits, there);
+    return s;
 }
 
+// f(step) over the wavefront's share of the workgroup's chunk, as often as asked.  kSteps: its steps where they stay in
+// registers; 0: any number of them, read again each time.
+template <int kSteps>
+struct Share {
+    const SortArgs& a;
+    int64_t start, share;
+    Place p[kSteps ? kSteps : 1];
+    Step step[kSteps ? kSteps : 1];
+    __device__ __forceinline__ explicit Share(const SortArgs& args) : a(args) {
+        share = a.chunk / kSortWaves;
+        start = blockIdx.x * a.chunk + threadIdx.x / kWave * share;
+        if constexpr (kSteps > 0)
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k) p[k] = fetch(start + k * kWave);
+    }
+    __device__ __forceinline__ void arrive() {
+        if constexpr (kSteps > 0)
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k) step[k] = made(p[k], start + k * kWave);
+    }
+    __device__ __forceinline__ Place fetch(int64_t at) const {
+        const int64_t i = at + threadIdx.x % kWave;
+        return i < a.T ? place_at(a, i) : Place{0, 0};
+    }
+    __device__ __forceinline__ Step made(Place p, int64_t at) const {
+        return step_of(p, at + threadIdx.x % kWave < a.T, a.shift, a.bits);
+    }
+    template <typename F>
+    __device__ __forceinline__ void each(F f) const {
+        if constexpr (kSteps > 0) {
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k) f(step[k]);
+        } else {
+            for (int64_t at = start; at < start + share && at < a.T; at += kWave) f(made(fetch(at), at));
+        }
+    }
+};
+
+template <int kSteps>
 __global__ __launch_bounds__(kSortThreads) void count_kernel(SortArgs a) {
     __shared__ uint32_t count[kMostBins];
     const uint32_t bins = 1u << a.bits;
+    Share<kSteps> mine(a);
     if (threadIdx.x < bins) count[threadIdx.x] = 0;
     if (!a.from) {  // what later kernels start from
-        if (blockIdx.x == 0 && threadIdx.x == 0) *a.longs = 0;
+        if (blockIdx.x == 0 && threadIdx.x == 0) {
+            a.found[0] = 0;
+            a.found[1] = static_cast<uint32_t>(a.T);
+        }
         if (a.present)
             for (int64_t v = (static_cast<int64_t>(blockIdx.x) * kSortThreads + threadIdx.x) * 16; v < a.ids.V;
                  v += static_cast<int64_t>(gridDim.x) * kSortThreads * 16)
                 *reinterpret_cast<uint4*>(a.present + v) = {0, 0, 0, 0};
     }
     __syncthreads();
-    each_place(a, [&](Place, uint32_t digit, uint64_t same, bool there) {
-        if (there && (same & ((uint64_t{1} << threadIdx.x % kWave) - 1)) == 0) atomicAdd(&count[digit], __popcll(same));
+    mine.arrive();
+    mine.each([&](const Step& s) {
+        if (s.leads()) atomicAdd(&count[s.digit], __popcll(s.same));
     });
     __syncthreads();
     if (threadIdx.x < bins) a.counts[blockIdx.x * bins + threadIdx.x] = count[threadIdx.x];
 }
 
+// Where each wavefront's places of each digit go: next[wave][digit] holds how many it has, and then where the first goes.  n: how many
+// of digit threadIdx.x there are in all, b: those of the workgroups before (threads below `bins`).
+__device__ __forceinline__ void places_of_digits(uint32_t (&next)[kSortWaves][kMostBins], uint32_t (&sums)[kSortWaves], uint32_t bins, uint32_t n, uint32_t b) {
+    const int wave = threadIdx.x / kWave;
+    const uint32_t upto = wave_inclusive_scan(threadIdx.x < bins ? n : 0u);
+    if (threadIdx.x % kWave == kWave - 1) sums[wave] = upto;
+    __syncthreads();
+    if (threadIdx.x < bins) {
+        uint32_t at = upto - n + b, c[kSortWaves];
+#pragma unroll
+        for (int w = 0; w < kSortWaves; ++w) c[w] = next[w][threadIdx.x];
+#pragma unroll
+        for (int w = 0; w < kMostBins / kWave; ++w) at += w < wave ? sums[w] : 0;
+#pragma unroll
+        for (int w = 0; w < kSortWaves; ++w) {
+            next[w][threadIdx.x] = at;
+            at += c[w];
+        }
+    }
+    __syncthreads();
+}
+
+// Where the place of a step goes; the counter of its digit moves on.
+__device__ __forceinline__ uint32_t take_place(uint32_t* next, const Step& s) {
+    const uint32_t at = next[s.digit];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (s.leads()) next[s.digit] = at + __popcll(s.same);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    return at + s.before();
+}
+
+template <int kSteps>
 __global__ __launch_bounds__(kSortThreads) void scatter_kernel(SortArgs a) {
     __shared__ uint32_t next[kSortWaves][kMostBins], before[kSortThreads], all[kSortThreads], sums[kSortWaves];
-    const uint32_t bins = 1u << a.bits, wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    const uint32_t bins = 1u << a.bits, wave = threadIdx.x / kWave;
+    Share<kSteps> mine(a);
     // all counts of a digit, and those of the workgroups before this one, by several threads
     const uint32_t digit = threadIdx.x & (bins - 1), groups = kSortThreads / bins, group = threadIdx.x / bins;
     uint32_t b = 0, n = 0;
-#pragma unroll 8
+#pragma unroll 16
     for (uint32_t k = group; k < static_cast<uint32_t>(a.blocks); k += groups) {
         const uint32_t c = a.counts[k * bins + digit];
         n += c;
@@ -92,43 +174,130 @@ __global__ __launch_bounds__(kSortThreads) void scatter_kernel(SortArgs a) {
     }
     before[threadIdx.x] = b;
     all[threadIdx.x] = n;
-    for (uint32_t k = threadIdx.x; k < kSortWaves * kMostBins; k += kSortThreads) (&next[0][0])[k] = 0;
+    for (uint32_t k = group; k < kSortWaves; k += groups) next[k][digit] = 0;
+    mine.arrive();
     __syncthreads();
-    each_place(a, [&](Place, uint32_t d, uint64_t same, bool there) {
-        if (there && (same & ((uint64_t{1} << lane) - 1)) == 0) next[wave][d] += __popcll(same);
+    mine.each([&](const Step& s) {
+        if (s.leads()) next[wave][s.digit] += __popcll(s.same);
     });
     if (threadIdx.x < bins)
         for (uint32_t g = 1; g < groups; ++g) {
             b += before[threadIdx.x + g * bins];
             n += all[threadIdx.x + g * bins];
         }
-    const uint32_t upto = wave_inclusive_scan(threadIdx.x < bins ? n : 0u);
-    if (lane == kWave - 1) sums[wave] = upto;
-    __syncthreads();
-    if (threadIdx.x < bins) {
-        uint32_t at = upto - n + b;
-        for (uint32_t w = 0; w < wave; ++w) at += sums[w];
-        for (int w = 0; w < kSortWaves; ++w) {
-            const uint32_t c = next[w][threadIdx.x];
-            next[w][threadIdx.x] = at;
-            at += c;
-        }
+    places_of_digits(next, sums, bins, n, b);
+    mine.each([&](const Step& s) {
+        const uint32_t at = take_place(next[wave], s);
+        if (!s.there) return;
+        a.to[at] = s.p;
+        if (!a.from && a.present && s.p.token < a.ids.V) a.present[s.p.token] = 1;
+    });
+}
+
+// The same in one kernel, where tokens and places are not too many: each workgroup takes kRange tokens, looks through all places for them, and counts those of lower tokens on the way, so that it knows where its own go.
+// A wavefront looks through a share of the places and lists what it finds, up to kList of them; with more it looks again.
+// 65536 places of 32000 tokens: measured beside the radix sort's two passes.
+constexpr int kRange = 256, kList = 384, kLook = 8;
+
+__global__ __launch_bounds__(kSortThreads) void order_kernel(SortArgs a) {
+    __shared__ uint32_t next[kSortWaves][kMostBins], sums[kSortWaves], lower;
+    __shared__ uint32_t list[kSortWaves][kList];  // place from the share's first on, and token from the range's first on in 8 bits
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+    const uint32_t lo = blockIdx.x * kRange, V = a.ids.V;
+    const uint32_t range = V - lo < kRange ? V - lo : kRange;
+    const int64_t share = (a.T + kSortThreads - 1) / kSortThreads * kWave, start = wave * share;
+    const int64_t end = start + share < a.T ? start + share : a.T;
+    for (uint32_t k = threadIdx.x / kRange; k < kSortWaves; k += kSortThreads / kRange) next[k][threadIdx.x % kRange] = 0;
+    if (threadIdx.x == 0) {
+        lower = 0;
+        if (blockIdx.x == 0) a.found[0] = 0;
     }
+    uint32_t below = 0, n = 0;
+    const auto look = [&](auto type) {
+        typedef decltype(type) Id;
+        const Id* ids = static_cast<const Id*>(a.ids.p);
+        const auto fetch = [&](int64_t at, Id (&id)[kLook]) {
+#pragma unroll
+            for (int k = 0; k < kLook; ++k) {
+                const int64_t i = at + k * kWave + lane;
+                id[k] = ids[i < end ? i : end - 1];
+            }
+        };
+        const auto one = [&](Id id, int64_t first, uint64_t there) {
+            const uint32_t low = static_cast<uint32_t>(id);
+            // (a negative number of 32 bits is above V; one of 64 has bits above the lower 32, like all that are too large)
+            if constexpr (sizeof(Id) == 8) there &= __ballot(static_cast<uint32_t>(static_cast<uint64_t>(id) >> 32) == 0);
+            below += __popcll(__ballot(low < lo) & there);
+            const uint64_t in = __ballot(low - lo < range) & there;
+            if (in == 0) return;
+            if (in >> lane & 1) {
+                const uint32_t to = n + __popcll(in & ((uint64_t{1} << lane) - 1));
+                if (to < kList) list[wave][to] = (static_cast<uint32_t>(first - start) + lane) << 8 | (low - lo);
+            }
+            n += __popcll(in);
+        };
+        const auto work = [&](int64_t at, const Id (&id)[kLook]) {
+            if (at + kLook * kWave <= end) {
+#pragma unroll
+                for (int k = 0; k < kLook; ++k) one(id[k], at + k * kWave, ~uint64_t{0});
+            } else {
+#pragma unroll
+                for (int k = 0; k < kLook; ++k) {
+                    const int64_t left = end - (at + k * kWave);
+                    if (left > 0) one(id[k], at + k * kWave, left < kWave ? (uint64_t{1} << left) - 1 : ~uint64_t{0});
+                }
+            }
+        };
+        for (int64_t at = start; at < end; at += kLook * kWave) {
+            Id id[kLook];
+            fetch(at, id);
+            work(at, id);
+        }
+    };
+    if (a.ids.wide) look(int64_t{});
+    else look(int32_t{});
+    // f(step) over what the wavefront has found, 64 at a time
+    const auto each = [&](auto f) {
+        if (n <= kList) {
+            for (uint32_t k = 0; k < n; k += kWave) {
+                const bool there = k + lane < n;
+                const uint32_t found = there ? list[wave][k + lane] : 0;
+                f(step_of({found & 255, static_cast<uint32_t>(start) + (found >> 8)}, there, 0, 8));
+            }
+        } else {
+            for (int64_t at = start; at < end; at += kWave) {
+                const int64_t i = at + lane;
+                const uint32_t code = i < end ? a.ids[i] - lo : kRange;
+                f(step_of({code, static_cast<uint32_t>(i)}, code < range, 0, 8));
+            }
+        }
+    };
     __syncthreads();
-    each_place(a, [&](Place p, uint32_t d, uint64_t same, bool there) {
-        if (!there) return;
-        const uint64_t lower = same & ((uint64_t{1} << lane) - 1);
-        const uint32_t at = next[wave][d];
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        if (lower == 0) next[wave][d] = at + __popcll(same);
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        a.to[at + __popcll(lower)] = p;
-        if (!a.from && a.present && p.token < a.ids.V) a.present[p.token] = 1;
+    if (lane == 0) atomicAdd(&lower, below);
+    each([&](const Step& s) {
+        if (s.leads()) next[wave][s.digit] += __popcll(s.same);
+    });
+    __syncthreads();
+    uint32_t count = 0;
+    if (threadIdx.x < kRange) {
+#pragma unroll
+        for (int w = 0; w < kSortWaves; ++w) count += next[w][threadIdx.x];
+        if (a.present && lo + threadIdx.x < V) a.present[lo + threadIdx.x] = count > 0;
+    }
+    places_of_digits(next, sums, kRange, count, lower);
+    if (blockIdx.x + 1 == gridDim.x && threadIdx.x == 0) {  // what is none is not listed
+        uint32_t all = lower;
+        for (int w = 0; w < kSortWaves; ++w) all += sums[w];
+        a.found[1] = all;
+    }
+    each([&](const Step& s) {
+        const uint32_t at = take_place(next[wave], s);
+        if (s.there) a.to[at] = {lo + s.p.token, s.p.t};
     });
 }
 
 // ----------------------------------------------------------------------------------------- sums
-constexpr int kPiece = 32, kAhead = 8, kSumThreads = 256;
+constexpr int kAhead = 8, kSumThreads = 256;
 
 struct SumArgs {
     const void* dY;
@@ -139,65 +308,72 @@ struct SumArgs {
     float scale;
     const Place* places;
     const uint8_t* present;
-    uint32_t *longs, *list;  // pieces in which a token of more than kPiece places starts
+    uint32_t *found, *list;  // how many tokens have more places than a piece, and how many are listed; the pieces where such tokens start
     float* partial;          // two rows a piece: of the token that it starts within, and of the long one that starts in it
     int64_t width;           // floats of such a row
     int64_t sum_blocks, blocks;  // that add up pieces, and with those that write zeros
     int zero_rows;               // of dE, for one of these
 };
 
-// The N columns of a lane: the row's last N where fewer are left, of which the first `skip` are another lane's.
-template <typename T, int N>
-__device__ __forceinline__ void add_to_row(T* row, int n, int64_t at, int skip, const float (&x)[N], bool accumulate) {
-    if (skip >= N) return;
-    float z[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) z[i] = x[i];
-    Raw<T, N> r;
-    if (skip == 0 && n >= N) {
-        if (accumulate) {
-            r.load(row + at);
-#pragma unroll
-            for (int i = 0; i < N; ++i) z[i] += r.get(i);
-        }
-        r.set(z);
-        r.store(row + at);
-        return;
+// Columns `from` .. `from` + N - 1 of a row of n: the row's last N where fewer are left, of which the first `skip` are another
+// lane's (all of them: the lane has none).
+template <int N>
+struct Columns {
+    int64_t from;
+    int skip, n;
+    Columns() = default;
+    __device__ __forceinline__ Columns(int64_t c, int width) : n(width) {
+        from = c + N <= n ? c : n > N ? n - N : 0;
+        skip = static_cast<int>(c - from < N ? c - from : N);
     }
+    template <bool kOnce, typename T>
+    __device__ __forceinline__ void load(const T* row, Raw<T, N>& x) const {
+        if (n >= N) x.template load_as<kOnce>(row + from);
+        else x.load_some(row, n);
+    }
+    template <bool kOnce, typename T>
+    __device__ __forceinline__ void store(T* row, const float (&x)[N]) const {
+        Raw<T, N> r;
+        r.set(x);
+        if (skip == 0 && n >= N) return r.template store_as<kOnce>(row + from);
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-        if (i >= skip && at + i < n) store_from_f32(row + at + i, accumulate ? z[i] + load_as_f32(row + at + i) : z[i]);
-}
+        for (int i = 0; i < N; ++i)
+            if (i >= skip && from + i < n) row[from + i] = r.element(i);
+    }
+};
 
-// Zeros in the rows of tokens that do not occur, kSumThreads to a row.
-template <typename TE>
+// Zeros in those of up to 64 rows whose tokens do not occur, kSumThreads to a row.
+template <typename TE, bool kOnce>
 __device__ __forceinline__ void zero_rows(const SumArgs& a, int64_t block) {
-    const int64_t first = block * a.zero_rows, end = first + a.zero_rows < a.V ? first + a.zero_rows : a.V;
-    for (int64_t v = first; v < end; ++v) {
-        if (a.present[v]) continue;
-        TE* row = static_cast<TE*>(a.dE) + v * a.ldde;
-        Raw<TE, 8> zero;
-        zero.zero();
-        for (int64_t c = threadIdx.x * 8; c < a.n; c += kSumThreads * 8) {
-            if (c + 8 <= a.n) zero.store(row + c);
+    constexpr int N = 16 / sizeof(TE);
+    const int64_t first = block * a.zero_rows, v = first + threadIdx.x % kWave;
+    uint64_t absent = __ballot(threadIdx.x % kWave < a.zero_rows && v < a.V && !a.present[v < a.V ? v : 0]);
+    Raw<TE, N> zero;
+    zero.zero();
+    for (; absent; absent &= absent - 1) {
+        TE* row = static_cast<TE*>(a.dE) + (first + __ffsll(static_cast<unsigned long long>(absent)) - 1) * a.ldde;
+        for (int64_t c = threadIdx.x * N; c < a.n; c += kSumThreads * N) {
+            if (c + N <= a.n) zero.template store_as<kOnce>(row + c);
             else zero.store_some(row + c, static_cast<int>(a.n - c));
         }
     }
 }
 
 // A wavefront's work: the columns of a tile in a piece.
-template <typename TY, typename TE, bool kAccumulate>
+template <typename TY, typename TE, int kPiece, bool kAccumulate, bool kIn, bool kOut>
 __device__ __forceinline__ void sum_piece(const SumArgs& a, int64_t item) {
-    constexpr int N = 16 / sizeof(TY);
+    // 16 bytes of dY a lane, and of dE at a time
+    constexpr int N = 16 / sizeof(TY), kEach = sizeof(TY) < sizeof(TE) ? 16 / sizeof(TE) : N, kGroups = N / kEach;
     const int lane = threadIdx.x % kWave;
     const int64_t piece = item / a.tiles;
     const int tile = static_cast<int>(item - piece * a.tiles);
     if (piece >= a.pieces) return;
     // the piece's places and as many behind it; a start is a place whose token is not the one before's
     const int64_t p0 = piece * kPiece;
-    const auto token_at = [&](int64_t i) { return i < 0 ? 0xFFFFFFFEu : i < a.T ? a.places[i].token : 0xFFFFFFFFu; };
+    const int64_t T = a.found[1];
+    const auto token_at = [&](int64_t i) { return i < 0 ? 0xFFFFFFFEu : i < T ? a.places[i].token : 0xFFFFFFFFu; };
     const int64_t mine = p0 + lane;
-    const Place here = mine < a.T ? a.places[mine] : Place{0xFFFFFFFFu, 0};
+    const Place here = mine < T ? a.places[mine] : Place{0xFFFFFFFFu, 0};
     const uint32_t left = token_at(mine - 1), back = token_at(p0 - 1 - lane);  // (back: lane l is l + 1 places before the piece)
     const uint64_t starts = __ballot(here.token != left);
     const uint32_t head = __builtin_amdgcn_readfirstlane(here.token);
@@ -228,64 +404,92 @@ __device__ __forceinline__ void sum_piece(const SumArgs& a, int64_t item) {
     }
     if (end > tokens) end = tokens;
     if (begin >= end) return;
-    if (tail < end && tile == 0 && lane == 0) a.list[atomicAdd(a.longs, 1u)] = static_cast<uint32_t>(piece);
+    if (tail < end && tile == 0 && lane == 0) a.list[atomicAdd(a.found, 1u)] = static_cast<uint32_t>(piece);
 
-    const int64_t c = (static_cast<int64_t>(tile) * kWave + lane) * N, at = c + N <= a.n ? c : a.n > N ? a.n - N : 0;
-    const int skip = static_cast<int>(c - at);
-    float sum[N];
+    // a lane's columns: kGroups times kEach side by side
+    Columns<kEach> at[kGroups];
 #pragma unroll
-    for (int i = 0; i < N; ++i) sum[i] = 0.f;
-    const TY* column = static_cast<const TY*>(a.dY) + at;
+    for (int g = 0; g < kGroups; ++g) at[g] = Columns<kEach>((static_cast<int64_t>(tile) * kGroups + g) * (kWave * kEach) + lane * kEach, a.n);
+    const auto some = [&](int g) { return g == 0 || (static_cast<int64_t>(tile) * kGroups + g) * (kWave * kEach) < a.n; };
+    float sum[kGroups][kEach];
+    const auto clear = [&] {
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+            for (int q = 0; q < kEach; ++q) sum[g][q] = 0.f;
+    };
+    clear();
+    const auto last_of_token = [&](int j) { return j + 1 == end || (starts >> (j + 1) & 1); };
+    const auto partly = [&](int j) { return j < first || j >= tail; };
+    const auto row_of = [&](int j) { return static_cast<TE*>(a.dE) + static_cast<uint32_t>(__builtin_amdgcn_readlane(here.token, j)) * a.ldde; };
     for (int i = begin; i < end; i += kAhead) {
-        Raw<TY, N> x[kAhead];
+        Raw<TY, kEach> x[kAhead][kGroups];
+        Raw<TE, kEach> was[kAccumulate ? kAhead : 1][kGroups];
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
-            const uint32_t t = __builtin_amdgcn_readlane(here.t, i + k < end ? i + k : end - 1);
-            if (a.n >= N) x[k].load(column + t * a.lddy);
-            else x[k].load_some(column + t * a.lddy, a.n);
+            const int j = i + k < end ? i + k : end - 1;
+            const TY* row = static_cast<const TY*>(a.dY) + static_cast<uint32_t>(__builtin_amdgcn_readlane(here.t, j)) * a.lddy;
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g)
+                if (some(g)) at[g].template load<kIn>(row, x[k][g]);
         }
+        if constexpr (kAccumulate)  // (the rows that are added to are on their way at the same time)
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                const int j = i + k;
+                if (j >= end || !last_of_token(j) || partly(j)) continue;
+                const TE* row = row_of(j);
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g)
+                    if (some(g)) at[g].template load<false>(row, was[k][g]);
+            }
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
             const int j = i + k;
             if (j >= end) break;
 #pragma unroll
-            for (int q = 0; q < N; ++q) sum[q] += x[k].get(q);
-            if (j + 1 < end && !(starts >> (j + 1) & 1)) continue;
-            // the token's last place here
-            if (j < first || j >= tail) {
-                float* out = a.partial + (2 * piece + (j >= tail ? 1 : 0)) * a.width + at;
+            for (int g = 0; g < kGroups; ++g)
+                if (some(g))
 #pragma unroll
-                for (int q = 0; q < N; ++q)
-                    if (q >= skip) out[q] = sum[q];
+                    for (int q = 0; q < kEach; ++q) sum[g][q] += x[k][g].get(q);
+            if (!last_of_token(j)) continue;
+            if (partly(j)) {
+                float* row = a.partial + (2 * piece + (j >= tail ? 1 : 0)) * a.width;
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g)
+                    if (some(g)) at[g].template store<false>(row, sum[g]);
             } else {
+                TE* row = row_of(j);
 #pragma unroll
-                for (int q = 0; q < N; ++q) sum[q] *= a.scale;
-                const uint32_t v = __builtin_amdgcn_readlane(here.token, j);
-                add_to_row<TE, N>(static_cast<TE*>(a.dE) + v * a.ldde, a.n, at, skip, sum, kAccumulate);
+                for (int g = 0; g < kGroups; ++g) {
+                    if (!some(g)) continue;
+#pragma unroll
+                    for (int q = 0; q < kEach; ++q) sum[g][q] = sum[g][q] * a.scale + (kAccumulate ? was[k][g].get(q) : 0.f);
+                    at[g].template store<kOut>(row, sum[g]);
+                }
             }
-#pragma unroll
-            for (int q = 0; q < N; ++q) sum[q] = 0.f;
+            clear();
         }
     }
 }
 
-template <typename TY, typename TE, bool kAccumulate>
+template <typename TY, typename TE, int kPiece, bool kAccumulate, bool kIn, bool kOut>
 __global__ __launch_bounds__(kSumThreads) void sum_kernel(SumArgs a) {
     for (int64_t block = blockIdx.x; block < a.blocks; block += gridDim.x) {
-        if (block >= a.sum_blocks) zero_rows<TE>(a, block - a.sum_blocks);
-        else sum_piece<TY, TE, kAccumulate>(a, block * (kSumThreads / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave));
+        if (block >= a.sum_blocks) zero_rows<TE, kOut>(a, block - a.sum_blocks);
+        else sum_piece<TY, TE, kPiece, kAccumulate, kIn, kOut>(a, block * (kSumThreads / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave));
     }
 }
 
 // The partial sums of a long token, 256 columns a workgroup at a time: each wavefront adds up a share of the pieces in order, and the
 // shares are added in order.
-constexpr int kJoinThreads = 512, kJoinWaves = kJoinThreads / kWave;
+constexpr int kJoinThreads = 256, kJoinWaves = kJoinThreads / kWave;
 
-template <typename TE, bool kAccumulate>
+template <typename TE, int kPiece, bool kAccumulate>
 __global__ __launch_bounds__(kJoinThreads) void join_kernel(SumArgs a) {
     __shared__ float4 part[kJoinWaves][kWave];
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    const int64_t tiles = (static_cast<int64_t>(a.n) + 255) / 256, items = *a.longs * tiles;
+    const int64_t tiles = (static_cast<int64_t>(a.n) + 255) / 256, items = a.found[0] * tiles, T = a.found[1];
     for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
         const int64_t piece = a.list[item / tiles];
         const int64_t c = item % tiles * 256 + lane * 4;
@@ -294,7 +498,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(SumArgs a) {
         int64_t more = 0;
         for (;; more += kWave) {
             const int64_t i = (piece + 1 + more + lane) * kPiece;
-            const uint64_t other = __ballot(i >= a.T || a.places[i].token != v);
+            const uint64_t other = __ballot(i >= T || a.places[i].token != v);
             if (other) {
                 more += __ffsll(static_cast<unsigned long long>(other)) - 1;
                 break;
@@ -340,10 +544,12 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(SumArgs a) {
 }
 
 // ------------------------------------------------------------------------------------ workspace
+constexpr int kSteps = 2;  // of a wavefront in a chunk of a sort over not too many places
+
 struct Room {
     int64_t chunk, pieces, width;
-    int bits, passes, blocks, tiles;
-    size_t places, counts, present, longs, list, partial, bytes;  // where each starts (two lists of places)
+    int bits, passes, blocks, piece;
+    size_t places, counts, present, found, list, partial, bytes;  // where each starts (two lists of places)
 };
 
 Room room_of(int64_t T, int64_t V, int64_t n) {
@@ -352,12 +558,13 @@ Room room_of(int64_t T, int64_t V, int64_t n) {
     while (V >> all) ++all;  // tokens 0 .. V - 1, and V for what is none
     r.passes = (all + kMostBits - 1) / kMostBits;
     r.bits = (all + r.passes - 1) / r.passes;
-    r.chunk = 2 * kSortThreads;
+    r.chunk = kSteps * kSortThreads;
     while ((T + r.chunk - 1) / r.chunk > 256) r.chunk *= 2;
     r.blocks = T > 0 ? static_cast<int>((T + r.chunk - 1) / r.chunk) : 1;
-    r.pieces = (T + kPiece - 1) / kPiece;
-    r.tiles = static_cast<int>((n + kWave * 4 - 1) / (kWave * 4));  // of 4 columns a lane; half as many of 8
-    r.width = (static_cast<int64_t>(r.tiles) * kWave * 4 + 511) / 512 * 512;
+    r.width = (n + 511) / 512 * 512;
+    // Short pieces where there is little to do: more wavefronts, and more partial sums.
+    r.piece = (T + 31) / 32 * ((n + 511) / 512) < 1024 ? 8 : 32;
+    r.pieces = (T + r.piece - 1) / r.piece;
     size_t at = 0;
     const auto take = [&](size_t bytes) {
         const size_t start = at;
@@ -367,30 +574,32 @@ Room room_of(int64_t T, int64_t V, int64_t n) {
     r.places = take(2 * static_cast<size_t>(T) * sizeof(Place));
     r.counts = take((static_cast<size_t>(r.blocks) << r.bits) * 4);
     r.present = take(static_cast<size_t>(V));
-    r.longs = take(4);
-    r.list = take((static_cast<size_t>(T) / kPiece + 1) * 4);
+    r.found = take(8);
+    r.list = take((static_cast<size_t>(T) / r.piece + 1) * 4);
     r.partial = take(2 * static_cast<size_t>(r.pieces) * r.width * 4);
     r.bytes = at;
     return r;
 }
 
-template <typename TY, typename TE>
-void launch_sums(SumArgs a, bool accumulate, hipStream_t s) {
+template <typename TY, typename TE, int kPiece, bool kAccumulate>
+void launch_sums(SumArgs a, hipStream_t s) {
     constexpr int N = 16 / sizeof(TY);
     a.tiles = static_cast<int>((static_cast<int64_t>(a.n) + kWave * N - 1) / (kWave * N));
     a.sum_blocks = (a.pieces * a.tiles + kSumThreads / kWave - 1) / (kSumThreads / kWave);
-    a.zero_rows = a.n >= 2048 ? 8 : 16384 / a.n < 256 ? 16384 / a.n : 256;
-    a.blocks = a.sum_blocks + (accumulate ? 0 : (a.V + a.zero_rows - 1) / a.zero_rows);
-    const unsigned blocks = static_cast<unsigned>(a.blocks < kMostBlocks ? a.blocks : kMostBlocks);
+    a.zero_rows = a.n >= 2048 ? 8 : 16384 / a.n < 64 ? 16384 / a.n : 64;
+    a.blocks = a.sum_blocks + (kAccumulate ? 0 : (a.V + a.zero_rows - 1) / a.zero_rows);
     const int64_t joins = (a.T / kPiece) * ((static_cast<int64_t>(a.n) + 255) / 256);
-    const unsigned grid = static_cast<unsigned>(joins < 4 * kUnits ? joins : 4 * kUnits);
-    if (accumulate) {
-        sum_kernel<TY, TE, true><<<blocks, kSumThreads, 0, s>>>(a);
-        if (grid) join_kernel<TE, true><<<grid, kJoinThreads, 0, s>>>(a);
-    } else {
-        sum_kernel<TY, TE, false><<<blocks, kSumThreads, 0, s>>>(a);
-        if (grid) join_kernel<TE, false><<<grid, kJoinThreads, 0, s>>>(a);
-    }
+    const auto grid = [](int64_t blocks, int64_t most) { return static_cast<unsigned>(blocks < most ? blocks : most); };
+    // The streaming hint, for dE where it is large and for dY beyond half the cache.  us with neither / the first / both, bf16 into
+    // 32000 rows, all with the hint on rows of zeros (8192 x 2048 into fp32 without it 73): 131072 x 4096 into bf16 335 / 326 / 314;
+    // into fp32 65536 x 512 68.5 / 57.0 / 68.3, 65536 x 1024 95.3 / 93.9 / 91.7, 65536 x 2048 150 / 148 / 146, 8192 x 1024 36.0 / 37.9 /
+    // 43.3, 8192 x 2048 59.2 / 63.2 / 77.7.
+    const bool out = static_cast<double>(a.V) * a.n * sizeof(TE) > 1 << 25, in = static_cast<double>(a.T) * a.n * sizeof(TY) > kStreamed;
+    const unsigned blocks = grid(a.blocks, kMostBlocks);
+    if (kPiece == 32 && in && out) sum_kernel<TY, TE, kPiece, kAccumulate, kPiece == 32, true><<<blocks, kSumThreads, 0, s>>>(a);
+    else if (out) sum_kernel<TY, TE, kPiece, kAccumulate, false, true><<<blocks, kSumThreads, 0, s>>>(a);
+    else sum_kernel<TY, TE, kPiece, kAccumulate, false, false><<<blocks, kSumThreads, 0, s>>>(a);
+    if (joins) join_kernel<TE, kPiece, kAccumulate><<<grid(joins, 8 * kUnits), kJoinThreads, 0, s>>>(a);
 }
 
 }  // namespace
@@ -405,20 +614,35 @@ grass_status launch_embed_backward(const void* dY, grass_dtype dt, int64_t lddy,
     char* base = static_cast<char*>(ws);
     Place* places = reinterpret_cast<Place*>(base + r.places);
     uint8_t* present = accumulate ? nullptr : reinterpret_cast<uint8_t*>(base + r.present);
-    uint32_t* longs = reinterpret_cast<uint32_t*>(base + r.longs);
+    uint32_t* found = reinterpret_cast<uint32_t*>(base + r.found);
     SortArgs sort{tokens(ids, idt, V), nullptr, places, T, r.chunk, 0, r.bits, r.blocks, reinterpret_cast<uint32_t*>(base + r.counts),
-                  present, longs};
-    const unsigned grid = static_cast<unsigned>(r.blocks);
-    for (int pass = 0; pass < r.passes; ++pass) {
-        sort.shift = pass * r.bits;
-        sort.from = pass == 0 ? nullptr : places + (pass - 1) % 2 * T;
-        sort.to = places + pass % 2 * T;
-        count_kernel<<<grid, kSortThreads, 0, s>>>(sort);
-        scatter_kernel<<<grid, kSortThreads, 0, s>>>(sort);
+                  present, found};
+    const int64_t ranges = (V + kRange - 1) / kRange;
+    if (T > 0 && ranges * T <= (1 << 21)) {
+        order_kernel<<<static_cast<unsigned>(ranges), kSortThreads, 0, s>>>(sort);
+    } else {
+        const unsigned grid = static_cast<unsigned>(r.blocks);
+        for (int pass = 0; pass < r.passes; ++pass) {
+            sort.shift = pass * r.bits;
+            sort.from = pass == 0 ? nullptr : places + (pass - 1) % 2 * T;
+            sort.to = places + pass % 2 * T;
+            if (r.chunk == kSteps * kSortThreads) {
+                count_kernel<kSteps><<<grid, kSortThreads, 0, s>>>(sort);
+                scatter_kernel<kSteps><<<grid, kSortThreads, 0, s>>>(sort);
+            } else {
+                count_kernel<0><<<grid, kSortThreads, 0, s>>>(sort);
+                scatter_kernel<0><<<grid, kSortThreads, 0, s>>>(sort);
+            }
+        }
     }
-    const SumArgs a{dY, dE, lddy, ldde, T, r.pieces, static_cast<int>(n), 0, static_cast<uint32_t>(V), scale, sort.to, present, longs,
+    const SumArgs a{dY, dE, lddy, ldde, T, r.pieces, static_cast<int>(n), 0, static_cast<uint32_t>(V), scale, sort.to, present, found,
                     reinterpret_cast<uint32_t*>(base + r.list), reinterpret_cast<float*>(base + r.partial), r.width, 0, 0, 0};
-    const auto go = [&](auto from, auto to) { launch_sums<decltype(from), decltype(to)>(a, accumulate, s); };
+    const auto go = [&](auto from, auto to) {
+        typedef decltype(from) TY;
+        typedef decltype(to) TE;
+        if (r.piece == 8) accumulate ? launch_sums<TY, TE, 8, true>(a, s) : launch_sums<TY, TE, 8, false>(a, s);
+        else accumulate ? launch_sums<TY, TE, 32, true>(a, s) : launch_sums<TY, TE, 32, false>(a, s);
+    };
     if (dt == GRASS_F32) gdt == GRASS_F32 ? go(float{}, float{}) : go(float{}, uint16_t{});
     else gdt == GRASS_F32 ? go(uint16_t{}, float{}) : go(uint16_t{}, uint16_t{});
     return launch_status();
