@@ -590,8 +590,8 @@ grass_status grass_embed_forward(const void* E, grass_dtype edt, int64_t V, int6
  * dY: T x n of dtype `dt`; dE: V x n of dtype `gdt`; they do not overlap.  Rows of tokens that do not
  * occur are zeros, or with accumulate neither read nor written; rows of dY whose ids[t] names no token are
  * not read.  The sums are fp32, in an order that depends on the token numbers and sizes alone, so
- * that equal calls give equal bits.  `ws` must hold grass_embed_backward_workspace(T, V, n) bytes,
- * 16-byte aligned.  T = 0 writes zeros, or with accumulate nothing; V, n >= 1; scale is finite.
+ * that equal calls give equal bits.  `ws` must hold grass_embed_backward_workspace(T, V, n) bytes (which
+ * grow with T, so that one workspace serves shorter batches, too), 16-byte aligned.  T = 0 writes zeros, or with accumulate nothing; V, n >= 1; scale is finite.
  * Errors: NULL, SHAPE (also an address that is not a multiple of its type's size), DTYPE, WORKSPACE. */
 size_t grass_embed_backward_workspace(int64_t T, int64_t V, int64_t n);
 grass_status grass_embed_backward(const void* dY, grass_dtype dt, int64_t lddy, const void* ids,
@@ -615,7 +615,7 @@ grass_status grass_embed_backward(const void* dY, grass_dtype dt, int64_t lddy, 
  * infinity rlog, entropy, logp (where the target names a token) and top_logp are NaN, and top_idx is
  * -1; other rows are not affected.
  * 0 <= top <= GRASS_LOGP_MOST_TOP and top <= V.  `ws` must hold grass_logp_forward_workspace(T, V, top,
- * dt) bytes, 16-byte aligned (NULL where that is 0).  Equal calls give equal bits.  T = 0 is a no-op; V >= 1.
+ * dt) bytes (which grow with T), 16-byte aligned (NULL where that is 0).  Equal calls give equal bits.  T = 0 is a no-op; V >= 1.
  * Errors: NULL (also one of a pair without the other), SHAPE (also an address that is not a multiple
  * of its type's size), DTYPE, WORKSPACE. */
 #define GRASS_LOGP_MOST_TOP 64

@@ -18,6 +18,9 @@ struct Tokens {
 };
 inline Tokens tokens(const void* p, grass_index idt, int64_t V) { return {p, idt == GRASS_I64, static_cast<uint32_t>(V)}; }
 
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945f;
+// scale log2(e), at most the largest number there is (0 times it is 0)
+__device__ __forceinline__ float scale_of_powers(float scale) { return fminf(scale * kLog2e, 3.40282347e38f); }
 // scale * (x - m) of two logits, also where the difference alone would pass the range of fp32.
 __device__ __forceinline__ float scaled_difference(float x, float m, float scale) { return 2.f * (scale * (0.5f * x - 0.5f * m)); }
 

@@ -260,9 +260,33 @@ def test_gradient_of_a_long_batch_and_wide_rows():
     assert bool(((dE.double() - want).abs() <= (count.view(-1, 1) + 2) * U * size).all())
 
 
+@pytest.mark.parametrize("T,V", [(530000, 700), (1100003, 70001), (600000, 1)])
+def test_gradient_of_more_tokens_than_workgroups_sort_at_a_time(T, V):
+    n = 5
+    dY, ids = draw((T, n), 1, F32), zipf(T, V, 2)
+    ids[::11] = -1
+    dE = backward(dY, ids, nan((V, n), F32))
+    row = torch.where(ids < 0, V, ids)
+    want, size = (torch.zeros((V + 1, n), dtype=torch.float64, device=DEV).index_add_(0, row, x.double())[:V] for x in (dY, dY.abs()))
+    count = row.bincount(minlength=V + 1)[:V].view(-1, 1)
+    assert bool(((dE.double() - want).abs() <= (count + 2) * U * size).all())
+    assert torch.equal(backward(dY, ids, nan((V, n), F32)), dE)
+
+
+def test_workspace_serves_shorter_batches():
+    V, n = 32000, 512
+    sizes = [grass.embed_backward_workspace(T, V, n) for T in (0, 1, 100, 2047, 4096, 32000, 32736, 32737, 65536, 524288, 524289, 2000000)]
+    assert sizes == sorted(sizes)
+    ws = grass.workspace(grass.embed_backward_workspace(40000, V, n))
+    for T in (32736, 5, 40000, 1000):
+        dY, ids = draw((T, n), T, BF16), zipf(T, V, 3)
+        dE = grass.embed_backward(dY, ids, nan((V, n), F32), ws)
+        assert torch.equal(dE, backward(dY, ids, nan((V, n), F32)))
+
+
 # ------------------------------------------------------------------- streams, graphs, checks
-def test_on_another_stream_and_in_a_graph():
-    T, V, n = 700, 90, 136
+@pytest.mark.parametrize("T,V,n", [(700, 90, 136), (40000, 3000, 136)])
+def test_on_another_stream_and_in_a_graph(T, V, n):
     E, dY = draw((V, n), 1, BF16), draw((T, n), 2, BF16)
     ids, ids2 = zipf(T, V, 3), whole((T,), 4, V)
     Y, dE, was = nan((T, n), BF16), nan((V, n), F32), draw((V, n), 5, F32)

@@ -283,6 +283,29 @@ def test_target_numbers_of_64_bits_are_not_cut():
     assert not backward(x, targets, out["rmax"], out["rlog"], torch.ones(5, device=DEV))[1:].any()
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("V", [70, 5000, 70001])
+@pytest.mark.parametrize("scale", [3e38, 1e30, 1e6, 1e-6, 1e-30, 1e-38])
+def test_temperatures_of_any_size(V, scale, dtype):
+    """Cold ones leave the largest logits alone (here with a tie), hot ones make all alike."""
+    x = draw((4, V), 1, dtype, 2.0)
+    x[1, V // 2] = x[1].max()
+    x[2] = x[2] * 1e30
+    x[3, 1:] = -INF
+    targets = torch.stack([x[0].argmax(), x[1].argmax(), x[2].argmin(), torch.zeros((), dtype=torch.int64, device=DEV)])
+    scale = float(np.float32(scale))
+    out = forward(x, targets, min(V, 4), scale)
+    check_forward(x, None, scale, {**out, "top_logp": None, "top_idx": None})
+    _, rlog, logp, H = ends_ref.logp_rows(to_f64(x), scale)
+    idx, val = ends_ref.alternatives(to_f64(x), logp, min(V, 4))
+    assert np.array_equal(out["top_idx"].cpu().numpy(), idx)
+    for got, want in ((out["logp"], ends_ref.given(logp, targets.cpu().numpy())), (out["top_logp"], val)):
+        beyond = (want < -3.3e38) & (to_f64(got) < -3.3e38)  # where fp32 ends
+        size = (264 + 3 * (H - rlog) + 9 * rlog).reshape(4, *[1] * (want.ndim - 1))
+        with np.errstate(all="ignore"):
+            assert near(torch.from_numpy(np.where(beyond, 0.0, to_f64(got))), np.where(beyond, 0.0, want), (size + 4 * np.abs(want)) * U)
+
+
 def test_gradient_against_differences():
     """Along random directions v, |v| <= 1, in fp32 through the kernels, over a step of 1/16 to both sides: (1/16)^2 / 6 of the
     third derivative is left.  For log p that is the third central moment of v, below 1; for the entropy the joint cumulant of x and
