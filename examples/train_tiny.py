@@ -1,6 +1,6 @@
 """A small language model trained with everything the package has: the linear layers of its MLP by GRASS
 steps on r of their rows, embedding, output head and gains by AdamW with 8-bit moments and clipping,
-the norms and their gradients in between.
+the norms and their gradients in between, the embedding lookup and the loss at its ends.
 
     python examples/train_tiny.py [steps]
 
@@ -16,7 +16,7 @@ import torch
 
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 from paper_2406_17660_amd import grass  # noqa: E402
-from paper_2406_17660_amd.dense import AdamW, NormLayer  # noqa: E402
+from paper_2406_17660_amd.dense import AdamW, Embedding, NormLayer, TokenLoss  # noqa: E402
 from paper_2406_17660_amd.layer import AdamHyper, GrassLayer  # noqa: E402
 
 DEV, BF16 = "cuda", torch.bfloat16
@@ -28,38 +28,35 @@ class TinyModel:
         g.manual_seed(seed)
         normal = lambda *shape: (torch.randn(shape, generator=g, device=DEV) * 0.05).to(BF16)  # noqa: E731
         self.T, self.vocab = T, vocab
-        self.E, self.head = normal(vocab, hidden), normal(vocab, hidden)
+        self.embedding, self.head = Embedding(normal(vocab, hidden), T), normal(vocab, hidden)
+        self.loss = TokenLoss(T, vocab, BF16)
+        self.dlogp = torch.full((T,), -1.0 / T, device=DEV)  # of the mean over the tokens
         self.up, self.down = normal(inner, hidden), normal(hidden, inner)
         self.norm1, self.norm2 = (NormLayer(hidden, T, BF16, kind) for kind in ("rms", "rms"))
-        self.dE = torch.zeros((vocab, hidden), device=DEV)
         self.dhead = torch.empty((vocab, hidden), device=DEV)
         self.ws_head = grass.workspace(grass.dense_workspace(T, vocab, hidden, grass.BF16))
         adam = AdamHyper(lr=3e-3)
         self.grass = {name: GrassLayer(m, n, r, T, BF16, "multi_norm", True, alpha=1.0, adam=adam, seed=seed + k)
                       for k, (name, (m, n)) in enumerate({"up": (inner, hidden), "down": (hidden, inner)}.items())}
-        self.adamw = AdamW([(self.E, self.dE), (self.head, self.dhead)] + self.norm1.parameters() + self.norm2.parameters(),
+        self.adamw = AdamW(self.embedding.parameters() + [(self.head, self.dhead)] + self.norm1.parameters() + self.norm2.parameters(),
                            adam, weight_decay=0.01, moments="q8", max_norm=1.0)
         self.t = 0
 
     def step(self, tokens, targets, refresh_every=20):
         """Forward pass, backward pass and update; returns the loss (on the device)."""
-        T = self.T
-        h0 = self.E[tokens]
+        h0 = self.embedding.forward(tokens)
         y1 = self.norm1.forward(h0)
         a = y1 @ self.up.t()
         act = torch.relu(a)
         y2 = self.norm2.forward(act @ self.down.t(), R=h0)
-        logp = torch.log_softmax((y2 @ self.head.t()).float(), 1)
-        loss = -logp.gather(1, targets.view(-1, 1)).mean()
+        loss = -self.loss.forward(y2 @ self.head.t(), targets).mean()
 
-        dlogits = logp.exp()
-        dlogits.scatter_add_(1, targets.view(-1, 1), torch.full((T, 1), -1.0, device=DEV))
-        dlogits = (dlogits / T).to(BF16)
+        dlogits = self.loss.backward(self.dlogp)
         grass.dense_grad(dlogits, y2, self.dhead, self.ws_head)
         dh1 = self.norm2.backward(dlogits @ self.head)
         da = (dh1 @ self.down) * (a > 0)
         dh0 = self.norm1.backward(da @ self.up, dR=dh1)
-        self.dE.zero_().index_add_(0, tokens, dh0.float())
+        self.embedding.backward(dh0)
 
         for name, dY, X, W in (("down", dh1, act, self.down), ("up", da, y1, self.up)):
             layer = self.grass[name]

@@ -1,5 +1,5 @@
-"""What a model has around its projected linear layers: the norms in front of them, and AdamW for the
-parameters that no projection covers (embeddings, output head, gains).
+"""What a model has around its projected linear layers: the norms in front of them, the embedding and the log
+probabilities at its two ends, and AdamW for the parameters that no projection covers (embeddings, output head, gains).
 
 Like `layer.py` this owns buffers and issues library calls in order; every step is a HIP kernel
 behind `grass.*`.
@@ -52,6 +52,64 @@ class NormLayer:
     def parameters(self):
         """(weight, gradient) pairs."""
         return [(self.gain, self.dgain)] + ([(self.bias, self.dbias)] if self.bias is not None else [])
+
+
+class Embedding:
+    """The rows of E (V x n) by token, times `scale`, for up to T tokens at a time; dE: their gradient (a new fp32 tensor
+    unless one is given: the head's, where it shares the weights).  Numbers outside 0 .. V - 1 are padding: rows of zeros,
+    and no gradient.  backward() goes by the token numbers of the forward pass before it, which are kept by reference."""
+
+    def __init__(self, E, T, scale=1.0, dE=None):
+        V, n = E.shape
+        self.E, self.T, self.scale, self.ids = E, T, scale, None
+        self.dE = torch.zeros((V, n), dtype=torch.float32, device=E.device) if dE is None else dE
+        self.ws = grass.workspace(grass.embed_backward_workspace(T, V, n), E.device)
+
+    def forward(self, ids, dtype=None):
+        """The tokens' rows in a new tensor of E's type, or of `dtype`."""
+        assert ids.shape[0] <= self.T
+        self.ids = ids
+        return grass.embed_forward(self.E, ids, torch.empty((ids.shape[0], self.E.shape[1]), dtype=dtype or self.E.dtype,
+                                                            device=self.E.device), self.scale)
+
+    def backward(self, dY, accumulate=False):
+        """self.dE from the gradient of what forward() gave; added to what it holds where accumulate is true."""
+        return grass.embed_backward(dY, self.ids, self.dE, self.ws, self.scale, accumulate)
+
+    def parameters(self):
+        """(weight, gradient) pairs."""
+        return [(self.E, self.dE)]
+
+
+class TokenLoss:
+    """Log probabilities of given tokens under up to T rows of V logits of type `dtype`, and the gradient of a loss made of
+    them.  scale: the inverse of a temperature.  backward() goes by the logits and targets of the forward pass before it, which
+    are kept by reference.  Targets outside 0 .. V - 1 are padding: log probability 0, and no gradient."""
+
+    def __init__(self, T, V, dtype, scale=1.0, device="cuda"):
+        self.T, self.scale = T, scale
+        f32 = dict(dtype=torch.float32, device=device)
+        self.logp, self.rmax, self.rlog, self.entropy = (torch.empty(T, **f32) for _ in range(4))
+        self.ws = grass.workspace(grass.logp_forward_workspace(T, V, 0, grass.F32 if dtype == torch.float32 else grass.BF16), device)
+        self.given = None
+
+    def forward(self, logits, targets, entropy=False):
+        """The targets' log probabilities (and the rows' entropies): views that the next forward pass writes over."""
+        T = logits.shape[0]
+        assert T <= self.T
+        self.given = logits, targets, entropy
+        logp, H = self.logp[:T], self.entropy[:T] if entropy else None
+        grass.logp_forward(logits, targets, logp, self.ws, self.scale, entropy=H, rmax=self.rmax[:T], rlog=self.rlog[:T])
+        return (logp, H) if entropy else logp
+
+    def backward(self, dlogp, dentropy=None, in_place=True):
+        """The gradient of the logits from that of logp (and of the entropies, if forward() gave them): written over the
+        logits, or into a new tensor."""
+        logits, targets, entropy = self.given
+        assert dentropy is None or entropy, "the forward pass left no entropies"
+        T = logits.shape[0]
+        return grass.logp_backward(logits, targets, self.rmax[:T], self.rlog[:T], dlogp, logits if in_place else torch.empty_like(logits),
+                                   self.scale, entropy=self.entropy[:T] if dentropy is not None else None, dentropy=dentropy)
 
 
 class AdamW:
