@@ -352,12 +352,10 @@ struct Columns {
     }
 };
 
-// Zeros in those of up to 64 rows whose tokens do not occur, kSumThreads to a row.
+// Zeros in those of up to 64 rows from `first` on whose bit in `absent` is set, kSumThreads to a row.
 template <typename TE, bool kOnce>
-__device__ __forceinline__ void zero_rows(const SumArgs& a, int64_t block) {
+__device__ __forceinline__ void zero_rows(const SumArgs& a, int64_t first, uint64_t absent) {
     constexpr int N = 16 / sizeof(TE);
-    const int64_t first = block * a.zero_rows, v = first + threadIdx.x % kWave;
-    uint64_t absent = __ballot(threadIdx.x % kWave < a.zero_rows && v < a.V && !a.present[v < a.V ? v : 0]);
     Raw<TE, N> zero;
     zero.zero();
     for (; absent; absent &= absent - 1) {
@@ -486,8 +484,87 @@ __device__ __forceinline__ void sum_piece(const SumArgs& a, int64_t item) {
 template <typename TY, typename TE, int kPiece, bool kAccumulate, bool kIn, bool kOut>
 __global__ __launch_bounds__(kSumThreads) void sum_kernel(SumArgs a) {
     for (int64_t block = blockIdx.x; block < a.blocks; block += gridDim.x) {
-        if (block >= a.sum_blocks) zero_rows<TE, kOut>(a, block - a.sum_blocks);
-        else sum_piece<TY, TE, kPiece, kAccumulate, kIn, kOut>(a, block * (kSumThreads / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave));
+        if (block >= a.sum_blocks) {
+            const int64_t first = (block - a.sum_blocks) * a.zero_rows, v = first + threadIdx.x % kWave;
+            zero_rows<TE, kOut>(a, first, __ballot(threadIdx.x % kWave < a.zero_rows && v < a.V && !a.present[v < a.V ? v : 0]));
+        } else sum_piece<TY, TE, kPiece, kAccumulate, kIn, kOut>(a, block * (kSumThreads / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave));
+    }
+}
+
+// Up to kFew places: a wavefront to each (and tile) looks at all of them, and the one at a token's first place adds up its rows.  One
+// launch, without an order: 64 or 256 places and 64 features, added, 13.1 and 14.9 -> 6.9 us, what the call takes the host; 256 places and
+// 4096 features 15.9 -> 6.9; 64 places into 32000 x 2048 fp32 56.7 -> 51.9, rows of zeros (5.0 TB/s).
+constexpr int kFew = 256;
+
+template <typename TY, typename TE, bool kAccumulate, bool kOut>
+__global__ __launch_bounds__(kSumThreads) void few_kernel(SumArgs a, Tokens ids) {
+    constexpr int N = 16 / sizeof(TY), kChunks = kFew / kWave;
+    const int lane = threadIdx.x % kWave, T = static_cast<int>(a.T);
+    uint32_t id[kChunks];
+#pragma unroll
+    for (int b = 0; b < kChunks; ++b) id[b] = b * kWave + lane < T ? ids[b * kWave + lane] : ids.V;
+    for (int64_t block = blockIdx.x; block < a.blocks; block += gridDim.x) {
+        if (block >= a.sum_blocks) {
+            const int64_t first = (block - a.sum_blocks) * a.zero_rows;
+            const int rows = static_cast<int>(a.V - first < a.zero_rows ? a.V - first : a.zero_rows);
+            uint64_t mine = 0;
+#pragma unroll
+            for (int b = 0; b < kChunks; ++b) mine |= id[b] >= first && id[b] < first + rows ? uint64_t{1} << (id[b] - first) : 0;
+            uint32_t low = static_cast<uint32_t>(mine), high = static_cast<uint32_t>(mine >> 32);
+#pragma unroll
+            for (int o = kWave / 2; o > 0; o >>= 1) {
+                low |= __shfl_xor(low, o, kWave);
+                high |= __shfl_xor(high, o, kWave);
+            }
+            const uint64_t present = static_cast<uint64_t>(__builtin_amdgcn_readfirstlane(high)) << 32 | static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(low));
+            zero_rows<TE, kOut>(a, first, ~present & (rows == 64 ? ~uint64_t{0} : (uint64_t{1} << rows) - 1));
+            continue;
+        }
+        const int64_t item = block * (kSumThreads / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+        const int place = static_cast<int>(item / a.tiles), tile = static_cast<int>(item % a.tiles);
+        if (place >= T) continue;
+        uint32_t v = ids.V;
+        uint64_t same[kChunks];
+#pragma unroll
+        for (int b = 0; b < kChunks; ++b)
+            if (place / kWave == b) v = __builtin_amdgcn_readlane(id[b], place % kWave);
+        bool earlier = v >= ids.V;
+#pragma unroll
+        for (int b = 0; b < kChunks; ++b) {
+            same[b] = __ballot(id[b] == v);
+            const int before = place - b * kWave;  // places of the chunk that come before this one
+            earlier |= (before >= kWave ? same[b] : before > 0 ? same[b] & ((uint64_t{1} << before) - 1) : 0) != 0;
+        }
+        if (earlier) continue;
+        const Columns<N> at((static_cast<int64_t>(tile) * kWave + lane) * N, a.n);
+        TE* const row = static_cast<TE*>(a.dE) + v * a.ldde;
+        Raw<TE, N> was;
+        if constexpr (kAccumulate) at.template load<false>(row, was);
+        float sum[N];
+#pragma unroll
+        for (int q = 0; q < N; ++q) sum[q] = 0.f;
+#pragma unroll
+        for (int b = 0; b < kChunks; ++b)
+            for (uint64_t left = same[b]; left;) {
+                Raw<TY, N> x[kAhead];
+                int count = 0;
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k)
+                    if (left) {
+                        const int64_t t = b * kWave + __ffsll(static_cast<unsigned long long>(left)) - 1;
+                        left &= left - 1;
+                        ++count;
+                        at.template load<false>(static_cast<const TY*>(a.dY) + t * a.lddy, x[k]);
+                    }
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k)
+                    if (k < count)
+#pragma unroll
+                        for (int q = 0; q < N; ++q) sum[q] += x[k].get(q);
+            }
+#pragma unroll
+        for (int q = 0; q < N; ++q) sum[q] = sum[q] * a.scale + (kAccumulate ? was.get(q) : 0.f);
+        at.template store<false>(row, sum);
     }
 }
 
@@ -596,20 +673,40 @@ Room room_of(int64_t T, int64_t V, int64_t n) {
     return r;
 }
 
-template <typename TY, typename TE, int kPiece, bool kAccumulate>
-void launch_sums(SumArgs a, hipStream_t s) {
+unsigned grid(int64_t blocks, int64_t most) { return static_cast<unsigned>(blocks < most ? blocks : most); }
+
+// Workgroups for so many pieces, and for rows of zeros.
+template <typename TY>
+void divide(SumArgs& a, int64_t pieces, bool accumulate) {
     constexpr int N = 16 / sizeof(TY);
     a.tiles = static_cast<int>((static_cast<int64_t>(a.n) + kWave * N - 1) / (kWave * N));
-    a.sum_blocks = (a.pieces * a.tiles + kSumThreads / kWave - 1) / (kSumThreads / kWave);
+    a.sum_blocks = (pieces * a.tiles + kSumThreads / kWave - 1) / (kSumThreads / kWave);
     a.zero_rows = a.n >= 2048 ? 8 : 16384 / a.n < 64 ? 16384 / a.n : 64;
-    a.blocks = a.sum_blocks + (kAccumulate ? 0 : (a.V + a.zero_rows - 1) / a.zero_rows);
+    a.blocks = a.sum_blocks + (accumulate ? 0 : (static_cast<int64_t>(a.V) + a.zero_rows - 1) / a.zero_rows);
+}
+
+// Whether the streaming hint goes with dE.
+template <typename TE>
+bool large(const SumArgs& a) { return static_cast<double>(a.V) * a.n * sizeof(TE) > 1 << 25; }
+
+template <typename TY, typename TE>
+void launch_few(SumArgs a, const Tokens& ids, bool accumulate, hipStream_t s) {
+    divide<TY>(a, a.T, accumulate);
+    const unsigned blocks = grid(a.blocks, kMostBlocks);
+    if (accumulate) few_kernel<TY, TE, true, false><<<blocks, kSumThreads, 0, s>>>(a, ids);
+    else if (large<TE>(a)) few_kernel<TY, TE, false, true><<<blocks, kSumThreads, 0, s>>>(a, ids);
+    else few_kernel<TY, TE, false, false><<<blocks, kSumThreads, 0, s>>>(a, ids);
+}
+
+template <typename TY, typename TE, int kPiece, bool kAccumulate>
+void launch_sums(SumArgs a, hipStream_t s) {
+    divide<TY>(a, a.pieces, kAccumulate);
     const int64_t joins = (a.T / kPiece) * ((static_cast<int64_t>(a.n) + 255) / 256);
-    const auto grid = [](int64_t blocks, int64_t most) { return static_cast<unsigned>(blocks < most ? blocks : most); };
     // The streaming hint, for dE where it is large and for dY beyond half the cache.  us with neither / the first / both, bf16 into
     // 32000 rows, all with the hint on rows of zeros (8192 x 2048 into fp32 without it 73): 131072 x 4096 into bf16 335 / 326 / 314;
     // into fp32 65536 x 512 68.5 / 57.0 / 68.3, 65536 x 1024 95.3 / 93.9 / 91.7, 65536 x 2048 150 / 148 / 146, 8192 x 1024 36.0 / 37.9 /
     // 43.3, 8192 x 2048 59.2 / 63.2 / 77.7.
-    const bool out = static_cast<double>(a.V) * a.n * sizeof(TE) > 1 << 25, in = static_cast<double>(a.T) * a.n * sizeof(TY) > kStreamed;
+    const bool out = large<TE>(a), in = static_cast<double>(a.T) * a.n * sizeof(TY) > kStreamed;
     const unsigned blocks = grid(a.blocks, kMostBlocks);
     if (kPiece == 32 && in && out) sum_kernel<TY, TE, kPiece, kAccumulate, kPiece == 32, true><<<blocks, kSumThreads, 0, s>>>(a);
     else if (out) sum_kernel<TY, TE, kPiece, kAccumulate, false, true><<<blocks, kSumThreads, 0, s>>>(a);
@@ -635,9 +732,9 @@ grass_status launch_embed_backward(const void* dY, grass_dtype dt, int64_t lddy,
     const int64_t ranges = (V + kRange - 1) / kRange;
     // One kernel does as much as there are ranges times places.  us of whole calls with it / with the radix sort, 64 bf16 features:
     // 32000 tokens 16384 places 24.4 / 45.6, 32768 39.5 / 45.7, 65536 51.9 / 52.8; 128000 tokens 16384 places 29.4 / 36.4, 65536 66.8 / 61.2.
-    if (T > 0 && T <= 32768 && ranges * T <= (1 << 23) && ranges <= 65536) {  // (a grid has fewer than 2^32 threads)
+    if (T > kFew && T <= 32768 && ranges * T <= (1 << 23) && ranges <= 65536) {  // (a grid has fewer than 2^32 threads)
         order_kernel<<<static_cast<unsigned>(ranges), kSortThreads, 0, s>>>(sort);
-    } else {
+    } else if (T > kFew) {
         const unsigned grid = static_cast<unsigned>(r.blocks);
         for (int pass = 0; pass < r.passes; ++pass) {
             sort.shift = pass * r.bits;
@@ -657,6 +754,7 @@ grass_status launch_embed_backward(const void* dY, grass_dtype dt, int64_t lddy,
     const auto go = [&](auto from, auto to) {
         typedef decltype(from) TY;
         typedef decltype(to) TE;
+        if (T <= kFew) return launch_few<TY, TE>(a, sort.ids, accumulate, s);
         if (r.piece == 8) accumulate ? launch_sums<TY, TE, 8, true>(a, s) : launch_sums<TY, TE, 8, false>(a, s);
         else accumulate ? launch_sums<TY, TE, 32, true>(a, s) : launch_sums<TY, TE, 32, false>(a, s);
     };

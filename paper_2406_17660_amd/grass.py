@@ -783,39 +783,56 @@ def grad_norm(plan, max_norm, out, ws):
 _INDEXES = {torch.int32: I32, torch.int64: I64}
 
 
-def _tokens(t, T):
+# The calls below also refuse tensors of another device than the current one, on whose stream they are issued.
+def _current_device():
+    return torch.cuda.current_device() if _device is None else _device()
+
+
+def _tokens(t, T, device):
     """(address, type) of T token numbers."""
-    assert t.is_cuda and t.shape == (T,) and t.is_contiguous(), "token numbers: one contiguous vector"
     code = _INDEXES.get(t.dtype)
     if code is None:
         raise TypeError(f"unsupported type of token numbers {t.dtype}")
+    assert t.get_device() == device and t.shape == (T,) and t.is_contiguous(), "token numbers: one contiguous vector"
     return t.data_ptr(), code
 
 
-def _here(*tensors):
-    """Refuses tensors of another device than the current one, whose stream a call is issued on."""
-    device = torch.cuda.current_device() if _device is None else _device()
-    for t in tensors:
-        assert t is None or t.get_device() == device, "tensors of the current device expected"
-
-
-def _rows(t):
-    """(address, rows, cols, leading dimension) of a device matrix whose rows, a single one too, are contiguous."""
+def _rows(t, device):
+    """(address, type, rows, cols, leading dimension) of a matrix whose rows, a single one too, are contiguous."""
     rows, cols = t.shape
     ld, step = t.stride()
-    assert t.is_cuda and (step == 1 or cols <= 1), "rows must be contiguous"
-    return t.data_ptr(), rows, cols, cols if rows <= 1 else ld
+    assert t.get_device() == device and (step == 1 or cols <= 1), "contiguous rows on the current device expected"
+    return t.data_ptr(), _dtype(t), rows, cols, cols if rows <= 1 else ld
+
+
+def _floats(tensors, shape, device):
+    """Addresses of fp32 tensors of one shape (None: none)."""
+    found, f32 = [], torch.float32
+    for t in tensors:
+        if t is None:
+            found.append(None)
+        else:
+            assert t.dtype is f32 and t.shape == shape and t.get_device() == device and t.is_contiguous(), "shapes or types differ"
+            found.append(t.data_ptr())
+    return found
+
+
+def _room(ws, device):
+    """Address and bytes of a workspace (None: none)."""
+    if ws is None:
+        return None, 0
+    assert ws.get_device() == device and ws.is_contiguous()
+    return ws.data_ptr(), ws.nbytes
 
 
 def embed_forward(E, ids, Y, scale=1.0):
     """Y[t, :] = scale * E[ids[t], :]; rows of zeros where ids[t] is outside the vocabulary."""
-    _here(E, ids, Y)
-    pE, V, n, lde = _rows(E)
-    pY, T, ny, ldy = _rows(Y)
+    device = _current_device()
+    pE, edt, V, n, lde = _rows(E, device)
+    pY, ydt, T, ny, ldy = _rows(Y, device)
     assert ny == n, "shapes differ"
-    pi, idt = _tokens(ids, T)
-    _check(lib().grass_embed_forward(pE, _dtype(E), V, n, lde, pi, idt, T, scale, pY, _dtype(Y), ldy, _stream()),
-           "grass_embed_forward")
+    pi, idt = _tokens(ids, T, device)
+    _check(lib().grass_embed_forward(pE, edt, V, n, lde, pi, idt, T, scale, pY, ydt, ldy, _stream()), "grass_embed_forward")
     return Y
 
 
@@ -825,14 +842,14 @@ def embed_backward_workspace(T, V, n) -> int:
 
 def embed_backward(dY, ids, dE, ws, scale=1.0, accumulate=False):
     """dE[v, :] = scale * (sum of the rows of dY whose token is v), added to what dE holds where accumulate is true."""
-    _here(dY, ids, dE, ws)
-    pY, T, n, lddy = _rows(dY)
-    pE, V, ne, ldde = _rows(dE)
+    device = _current_device()
+    pY, dt, T, n, lddy = _rows(dY, device)
+    pE, gdt, V, ne, ldde = _rows(dE, device)
     assert ne == n, "shapes differ"
-    pi, idt = _tokens(ids, T)
-    wp, wb = _ws(ws)
-    _check(lib().grass_embed_backward(pY, _dtype(dY), lddy, pi, idt, T, V, n, scale, int(bool(accumulate)), pE, _dtype(dE),
-                                      ldde, wp, wb, _stream()), "grass_embed_backward")
+    pi, idt = _tokens(ids, T, device)
+    wp, wb = _room(ws, device)
+    _check(lib().grass_embed_backward(pY, dt, lddy, pi, idt, T, V, n, scale, 1 if accumulate else 0, pE, gdt, ldde, wp, wb,
+                                      _stream()), "grass_embed_backward")
     return dE
 
 
@@ -844,35 +861,35 @@ def logp_forward(logits, targets, logp, ws, scale=1.0, entropy=None, rmax=None, 
     """Log probabilities of the targets under the logits' rows (targets and logp: None where not wanted), the rows'
     entropies, what the backward pass needs of them (rmax, rlog: T floats), and the alternatives of largest
     probability with their log probabilities (top_idx int32, top_logp: T x top)."""
-    _here(logits, targets, logp, ws, entropy, rmax, rlog, top_logp, top_idx)
-    pl, T, V, ldl = _rows(logits)
-    f32 = torch.float32
-    pt, idt = (None, I32) if targets is None else _tokens(targets, T)
-    plogp, pent, pmax, plog = (None if v is None else _vector(v, T, f32) for v in (logp, entropy, rmax, rlog))
+    device = _current_device()
+    pl, dt, T, V, ldl = _rows(logits, device)
+    pt, idt = (None, I32) if targets is None else _tokens(targets, T, device)
+    plogp, pent, pmax, plog = _floats((logp, entropy, rmax, rlog), (T,), device)
     top, ptl, pti = 0, None, None
     if top_idx is not None:
-        top = top_idx.shape[1]
-        assert top_idx.shape == top_logp.shape == (T, top) and top_idx.dtype is torch.int32 and top_logp.dtype is f32
-        assert top_idx.is_cuda and top_logp.is_cuda and top_idx.is_contiguous() and top_logp.is_contiguous()
-        if top:
-            ptl, pti = top_logp.data_ptr(), top_idx.data_ptr()
-    wp, wb = _ws(ws)
-    _check(lib().grass_logp_forward(pl, _dtype(logits), T, V, ldl, pt, idt, scale, plogp, pent, pmax, plog, top, ptl, pti, wp,
-                                    wb, _stream()), "grass_logp_forward")
+        rows, top = top_idx.shape
+        assert rows == T and top_idx.dtype is torch.int32 and top_idx.get_device() == device and top_idx.is_contiguous()
+        ptl, = _floats((top_logp,), (T, top), device)
+        pti = top_idx.data_ptr() if top else None
+        ptl = ptl if top else None
+    else:
+        assert top_logp is None, "top_logp and top_idx go together"
+    wp, wb = _room(ws, device)
+    _check(lib().grass_logp_forward(pl, dt, T, V, ldl, pt, idt, scale, plogp, pent, pmax, plog, top, ptl, pti, wp, wb, _stream()),
+           "grass_logp_forward")
     return logp
 
 
 def logp_backward(logits, targets, rmax, rlog, dlogp, dlogits, scale=1.0, entropy=None, dentropy=None):
     """The gradient of the logits from those of logp and entropy (None: zeros); dlogits may be logits."""
-    _here(logits, targets, rmax, rlog, dlogp, dlogits, entropy, dentropy)
-    pl, T, V, ldl = _rows(logits)
-    pd, Td, Vd, lddl = _rows(dlogits)
-    assert (Td, Vd) == (T, V) and dlogits.dtype is logits.dtype, "shapes or types differ"
-    f32 = torch.float32
-    pt, idt = (None, I32) if targets is None else _tokens(targets, T)
-    pmax, plog, pdlogp, pent, pdent = (None if v is None else _vector(v, T, f32) for v in (rmax, rlog, dlogp, entropy, dentropy))
-    _check(lib().grass_logp_backward(pl, _dtype(logits), T, V, ldl, pt, idt, scale, pmax, plog, pdlogp, pent, pdent, pd, lddl,
-                                     _stream()), "grass_logp_backward")
+    device = _current_device()
+    pl, dt, T, V, ldl = _rows(logits, device)
+    pd, ddt, Td, Vd, lddl = _rows(dlogits, device)
+    assert Td == T and Vd == V and ddt == dt, "shapes or types differ"
+    pt, idt = (None, I32) if targets is None else _tokens(targets, T, device)
+    pmax, plog, pdlogp, pent, pdent = _floats((rmax, rlog, dlogp, entropy, dentropy), (T,), device)
+    _check(lib().grass_logp_backward(pl, dt, T, V, ldl, pt, idt, scale, pmax, plog, pdlogp, pent, pdent, pd, lddl, _stream()),
+           "grass_logp_backward")
     return dlogits
 
 
