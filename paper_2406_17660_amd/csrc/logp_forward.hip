@@ -165,6 +165,32 @@ __device__ __forceinline__ void rank_keys(const uint64_t* keys, int* ranks, int 
     for (int r = count + lane; r < top; r += threads) out(r, uint64_t{0});
 }
 
+// Leaves the keys of the `top` largest logits, and of those that equal the last of them, of `count` in LDS: comparing all with all would
+// take the square of their number.  The last one's value is found bit by bit, by every wavefront for itself.
+template <typename S>
+__device__ __forceinline__ int keep_best(uint64_t* keys, int& found, int count, int top, int lane) {
+    uint32_t value = 0;
+    for (uint32_t bit = 0x80000000u; bit; bit >>= 1) {
+        int n = 0;
+        for (int i = threadIdx.x % kWave; i - static_cast<int>(threadIdx.x % kWave) < count; i += kWave)
+            n += __popcll(__ballot(i < count && static_cast<uint32_t>(keys[i < count ? i : 0] >> 32) >= (value | bit)));
+        if (n >= top) value |= bit;
+        if (n == top) break;
+    }
+    constexpr int kMine = S::kCap / S::TPR;
+    uint64_t mine[kMine];
+#pragma unroll
+    for (int k = 0; k < kMine; ++k) mine[k] = lane + k * S::TPR < count ? keys[lane + k * S::TPR] : 0;
+    Group<S>::sync();
+    if (lane == 0) found = 0;
+    Group<S>::sync();
+#pragma unroll
+    for (int k = 0; k < kMine; ++k)
+        if (static_cast<uint32_t>(mine[k] >> 32) >= value && mine[k]) keys[atomicAdd(&found, 1)] = mine[k];
+    Group<S>::sync();
+    return found;
+}
+
 // A row, or a part of one: where it starts, how many logits it has, and the token of the first.
 template <typename T, typename S>
 struct Piece {
@@ -209,7 +235,7 @@ __global__ __launch_bounds__(S::B) __attribute__((amdgpu_waves_per_eu(8))) void 
     typedef Raw<T, N> Vector;
     __shared__ float2 room[2][G::kWaves];
     __shared__ uint64_t keys[S::kRows][kTop ? S::kCap : 1];
-    __shared__ float sets[kWave];
+    __shared__ float sets[2 * kWave];
     __shared__ int found[S::kRows], counts[G::kWaves], ranks[S::kRows][kTop ? S::kCap : 1];
     const int lane = threadIdx.x % TPR, wave0 = __builtin_amdgcn_readfirstlane(lane);
     const int group = S::kRows == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
@@ -243,39 +269,55 @@ __global__ __launch_bounds__(S::B) __attribute__((amdgpu_waves_per_eu(8))) void 
 #pragma unroll
         for (int v = 0; v < V; ++v)
             if (some(v)) row.mask(v, masking, x[v]);
-        float m = -INFINITY;
+        // The largest logit, of kSets sets for each lane of a wavefront where there are alternatives.
+        constexpr int kSets = !kTop ? 1 : TPR > kWave ? 2 : V < 2 ? V : 2, kOwn = TPR > kWave ? 1 : kSets;
+        float q[kSets];
+#pragma unroll
+        for (int k = 0; k < kSets; ++k) q[k] = -INFINITY;
 #pragma unroll
         for (int v = 0; v < V; ++v)
             if (some(v))
 #pragma unroll
-                for (int i = 0; i < N; i += 2) m = max3(m, x[v].get(i), x[v].get(i + 1));
+                for (int i = 0; i < N; i += 2) q[v % kOwn] = max3(q[v % kOwn], x[v].get(i), x[v].get(i + 1));
+        float m = q[0];
+#pragma unroll
+        for (int k = 1; k < kOwn; ++k) m = fmaxf(m, q[k]);
         const float own = m;
         float least = -INFINITY;
         const auto larger = [](float p, float q) { return fmaxf(p, q); };
         const auto plus = [](float p, float q) { return p + q; };
         if constexpr (kTop) {
-            // The threads in 64 sets: as many as `top` of these have a logit not below the `top`-th largest of their maxima, so that
-            // no alternative is below it, and few other logits are above.  It is found bit by bit (down to some, which is low enough).
-            constexpr int kSet = TPR / kWave, kBits = sizeof(T) == 2 ? 16 : 20;
-            over_lanes([&](auto step) {
-                constexpr int kStep = decltype(step)::value;
-                if constexpr ((1 << kStep) < kSet) m = fold<kStep>(m, larger);
-            });
-            if constexpr (kSet > 1) {
+            // As many of the sets as `top` have a logit not below the `top`-th largest of their maxima, so that no alternative is
+            // below it; and with twice as many sets as alternatives or more, few other logits are above: 64 sets left 300 of 32000
+            // for 64 alternatives, 128 leave 90.  It is found bit by bit (down to some, which is low enough).
+            if constexpr (TPR > kWave) {
+                constexpr int kSet = TPR / (kSets * kWave);  // threads
+                over_lanes([&](auto step) {
+                    constexpr int kStep = decltype(step)::value;
+                    if constexpr ((1 << kStep) < kSet) m = fold<kStep>(m, larger);
+                });
                 if (lane % kSet == 0) sets[lane / kSet] = m;
                 G::sync();
-                m = sets[threadIdx.x % kWave];
+#pragma unroll
+                for (int k = 0; k < kSets; ++k) {
+                    q[k] = sets[k * kWave + threadIdx.x % kWave];
+                    m = fmaxf(m, q[k]);
+                }
             }
-            const uint32_t order = order_of(m);
-            uint32_t bound = 0;
+            constexpr int kBits = sizeof(T) == 2 ? 16 : 20;
+            uint32_t order[kSets], bound = 0;
+#pragma unroll
+            for (int k = 0; k < kSets; ++k) order[k] = order_of(q[k]);
             for (uint32_t bit = 0x80000000u; bit >> (32 - kBits); bit >>= 1) {
-                const int n = __popcll(__ballot(order >= (bound | bit)));
+                int n = 0;
+#pragma unroll
+                for (int k = 0; k < kSets; ++k) n += __popcll(__ballot(order[k] >= (bound | bit)));
                 if (n >= a.top) bound |= bit;
-                if (n == a.top) break;
+                if (n == a.top && n < kSets * kWave) break;  // (where all sets are alternatives', many a bound is below all)
             }
             if (bound > kMasked) least = logit_of(bound);
             over_lanes([&](auto step) { m = fold<decltype(step)::value>(m, larger); });
-            if constexpr (kSet == 1) G::sync();  // (found is 0 for all)
+            if constexpr (TPR == kWave) G::sync();  // (found is 0 for all)
         } else {
             float none = 0.f;
             over_lanes([&](auto step) { m = fold<decltype(step)::value>(m, larger); });
@@ -379,6 +421,8 @@ __global__ __launch_bounds__(S::B) __attribute__((amdgpu_waves_per_eu(8))) void 
             G::sync();
             count = found[group];
         }
+        if constexpr (kTop)
+            if (count > 2 * a.top) count = keep_best<S>(keys[group], found[group], count, a.top, lane);
         if (a.parts == 1) {
             const Row out(a, z, t, given, target < a.targets.V, lane);
             if constexpr (kTop)
