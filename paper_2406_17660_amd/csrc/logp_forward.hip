@@ -289,7 +289,7 @@ __global__ __launch_bounds__(S::B) __attribute__((amdgpu_waves_per_eu(8))) void 
         if constexpr (kTop) {
             // As many of the sets as `top` have a logit not below the `top`-th largest of their maxima, so that no alternative is
             // below it; and with twice as many sets as alternatives or more, few other logits are above: 64 sets left 300 of 32000
-            // for 64 alternatives, 128 leave 90.  It is found bit by bit (down to some, which is low enough).
+            // for 64 alternatives, 128 leave 90.  It is found bit by bit (down to some, below which hardly any differ).
             if constexpr (TPR > kWave) {
                 constexpr int kSet = TPR / (kSets * kWave);  // threads
                 over_lanes([&](auto step) {
@@ -315,7 +315,12 @@ __global__ __launch_bounds__(S::B) __attribute__((amdgpu_waves_per_eu(8))) void 
                 if (n >= a.top) bound |= bit;
                 if (n == a.top && n < kSets * kWave) break;  // (where all sets are alternatives', many a bound is below all)
             }
-            if (bound > kMasked) least = logit_of(bound);
+            if (bound > kMasked) {  // the least of the maxima that are not below it
+                least = INFINITY;
+#pragma unroll
+                for (int k = 0; k < kSets; ++k) least = order[k] >= bound ? fminf(least, q[k]) : least;
+                over_lanes([&](auto step) { least = fold<decltype(step)::value>(least, [](float p, float q) { return fminf(p, q); }); });
+            }
             over_lanes([&](auto step) { m = fold<decltype(step)::value>(m, larger); });
             if constexpr (TPR == kWave) G::sync();  // (found is 0 for all)
         } else {
@@ -381,9 +386,10 @@ __global__ __launch_bounds__(S::B) __attribute__((amdgpu_waves_per_eu(8))) void 
         const Sums z{m, s, u * back - off * s};
         int count = kTop ? found[group] : 0;
         if (kTop && count > S::kCap) {
-            // More logits at the bound and above than there is room for, as where many are alike: the value of the last
-            // alternative, then its token among equals, bit by bit.
-            // (Read again: with the row's registers in these loops others would not do.)
+            // More logits at the bound and above than there is room for, as where many are alike.  Those above it may be enough; else
+            // the value of the last alternative is found, where it is not the bound, and its token among equals, bit by bit.
+            // (Read again: with the row's registers in these loops others would not do.  Looking for the token in one vector at a
+            // time takes half the time here and more registers, 51 us for 39 at 1025 x 50001; as a function of its own 45.)
             const int place = lane_again();
             const auto each = [&](auto f) {
 #pragma unroll 1
@@ -403,14 +409,14 @@ __global__ __launch_bounds__(S::B) __attribute__((amdgpu_waves_per_eu(8))) void 
             };
             uint32_t value = order_of(least);
             int above = how_many([&](uint32_t q, int) { return q > value; });
-            if (above >= a.top) {
+            if (above > S::kCap) {
                 value = 0;
                 for (uint32_t bit = 0x80000000u; bit; bit >>= 1)
                     if (how_many([&](uint32_t q, int) { return q >= (value | bit); }) >= a.top) value |= bit;
                 above = how_many([&](uint32_t q, int) { return q > value; });
             }
-            int last = 0;
-            for (int bit = 1 << (31 - __clz(a.V)); bit; bit >>= 1)
+            int last = above < a.top ? 0 : -1;
+            for (int bit = above < a.top ? 1 << (31 - __clz(a.V)) : 0; bit; bit >>= 1)
                 if (how_many([&](uint32_t q, int j) { return q == value && j < (last | bit); }) < a.top - above) last |= bit;
             if (lane == 0) found[group] = 0;
             G::sync();
