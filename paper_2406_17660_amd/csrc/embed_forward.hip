@@ -1,8 +1,8 @@
 // grass_embed_forward: rows of the embedding by token.
 //
 // Bound by memory: Y is written once, and a row of E is read from memory once and from the cache for the other
-// places of its token.  Measured: 131072 x 4096 bf16 from 32000 rows 286 us (1.07 GB written and 0.32 read, 4.9 TB/s, as a copy of
-// that size; two vectors a thread 301, eight 312, without the streaming hint 304, with it on E 357); 131072 x 1024 56 us.
+// places of its token.  Measured: 131072 x 4096 bf16 from 32000 rows 286 us (1.07 GB written and, as eight L2 caches fetch
+// the frequent rows, 0.65 read: 6.1 TB/s; two vectors a thread 301, eight 312, without the streaming hint 304, with it on E 357); 131072 x 1024 56 us.
 #include <type_traits>
 
 #include "elem.hpp"

@@ -1,7 +1,7 @@
 // grass_logp_forward: log probabilities of given tokens, entropies and alternatives.
 //
-// Measured: 32768 x 32000 bf16 303 us (6.9 TB/s); 256 x 128000 fp32 with entropies and 20 alternatives 40 (without alternatives
-// 27), 1025 x 50001 bf16 in any position with 5 alternatives 40; one row of 32000 bf16 with 20 alternatives 9.6 (kernel 8.8).
+// Measured: 32768 x 32000 bf16 303 us (7.0 TB/s); 256 x 128000 fp32 with entropies and 20 alternatives 41 (without alternatives
+// 27), 1025 x 50001 bf16 in any position with 5 alternatives 39; one row of 32000 bf16 with 20 alternatives 10.0 (kernel 9.3).
 //
 // Bound by memory: a row is read once and stays in the registers of the threads that share it, for its maximum, its
 // sums and its alternatives.  With c = scale log2(e) and d = (x - rmax) c, s = sum 2^d and u = sum 2^d d give
