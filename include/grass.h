@@ -591,7 +591,8 @@ grass_status grass_embed_forward(const void* E, grass_dtype edt, int64_t V, int6
  * occur are zeros, or with accumulate neither read nor written; rows of dY whose ids[t] names no token are
  * not read.  The sums are fp32, in an order that depends on the token numbers and sizes alone, so
  * that equal calls give equal bits.  `ws` must hold grass_embed_backward_workspace(T, V, n) bytes (which
- * grow with T, so that one workspace serves shorter batches, too), 16-byte aligned.  T = 0 writes zeros, or with accumulate nothing; V, n >= 1; scale is finite.
+ * grow with T, so that one workspace serves shorter batches, too), 16-byte aligned.  T = 0 writes zeros,
+ * or with accumulate nothing; V, n >= 1; scale is finite.
  * Errors: NULL, SHAPE (also an address that is not a multiple of its type's size), DTYPE, WORKSPACE. */
 size_t grass_embed_backward_workspace(int64_t T, int64_t V, int64_t n);
 grass_status grass_embed_backward(const void* dY, grass_dtype dt, int64_t lddy, const void* ids,
@@ -615,7 +616,8 @@ grass_status grass_embed_backward(const void* dY, grass_dtype dt, int64_t lddy, 
  * infinity rlog, entropy, logp (where the target names a token) and top_logp are NaN, and top_idx is
  * -1; other rows are not affected.
  * 0 <= top <= GRASS_LOGP_MOST_TOP and top <= V.  `ws` must hold grass_logp_forward_workspace(T, V, top,
- * dt) bytes (which grow with T), 16-byte aligned (NULL where that is 0).  Equal calls give equal bits.  T = 0 is a no-op; V >= 1.
+ * dt) bytes (which grow with T), 16-byte aligned (NULL where that is 0).  Equal calls give equal bits.
+ * T = 0 is a no-op; V >= 1.
  * Errors: NULL (also one of a pair without the other), SHAPE (also an address that is not a multiple
  * of its type's size), DTYPE, WORKSPACE. */
 #define GRASS_LOGP_MOST_TOP 64
@@ -631,7 +633,8 @@ grass_status grass_logp_forward(const void* logits, grass_dtype dt, int64_t T, i
  * rounded once to `dt`.  dlogp, dentropy: T floats, the gradients of logp and entropy; NULL: zeros (targets
  * may then be NULL, too; entropy is read only beside dentropy).  A row whose target names no token takes no
  * part in the first term.  A row without either term (dentropy[t] and dlogp[t] 0, or no token) is
- * zeros and is not read, whatever it holds; a row that is all masked is zeros.
+ * zeros and is not read, whatever it holds; a row that is all masked is zeros.  scale *
+ * (|dlogp[t]| + 32 |dentropy[t]|) is to be within the range of fp32: in a row where it is not, values may be NaN.
  * dlogits may be logits (the same address and leading dimension); other overlaps are not allowed.
  * T = 0 is a no-op; V >= 1.
  * Errors: NULL, SHAPE (also an address that is not a multiple of its type's size), DTYPE. */

@@ -98,7 +98,7 @@ def backward(x, targets, rmax, rlog, dlogp, scale=1.0, entropy=None, dentropy=No
                                dentropy=dentropy)
 
 
-def check_backward(x, targets, rmax, rlog, dlogp, scale, entropy, dentropy, dx):
+def check_backward(x, targets, rmax, rlog, dlogp, scale, entropy, dentropy, dx, steps=4, least=TINY):
     T = x.shape[0]
     f = lambda v: np.zeros(T) if v is None else to_f64(v)  # noqa: E731
     ids = np.full(T, -1) if targets is None or dlogp is None else targets.cpu().numpy().astype(np.int64)
@@ -106,7 +106,7 @@ def check_backward(x, targets, rmax, rlog, dlogp, scale, entropy, dentropy, dx):
     want, l, p = ends_ref.logp_backward(to_f64(x), ids, scale, m, r, g, H, h)
     with np.errstate(all="ignore"):
         arg = np.abs(l + r[:, None]) + np.abs(r)[:, None]
-        rel = (4 * arg + 8) * U
+        rel = (steps * arg + 8) * U
         lH = np.abs(l) + np.abs(H)[:, None]
         size = np.abs(g)[:, None] * (p * rel + 2 * U * p) + np.abs(h)[:, None] * p * (lH * (rel + 4 * U) + 4 * U * (arg + lH))
         size = np.where(p == 0, 0.0, size)
@@ -114,7 +114,7 @@ def check_backward(x, targets, rmax, rlog, dlogp, scale, entropy, dentropy, dx):
         size[there, ids[there]] += 4 * U * np.abs(g[there])
         size = size * scale + 2 * U * np.abs(want)
         half = torch.finfo(x.dtype).eps / 2 if x.dtype == BF16 else 0.0
-        off = size + half * (np.abs(want) + size) + TINY * (1 + np.abs(g) + np.abs(h))[:, None]
+        off = size + half * (np.abs(want) + size) + least * (1 + np.abs(g) + np.abs(h))[:, None]
     assert near(dx, want, off)
 
 
@@ -304,6 +304,24 @@ def test_temperatures_of_any_size(V, scale, dtype):
         size = (264 + 3 * (H - rlog) + 9 * rlog).reshape(4, *[1] * (want.ndim - 1))
         with np.errstate(all="ignore"):
             assert near(torch.from_numpy(np.where(beyond, 0.0, to_f64(got))), np.where(beyond, 0.0, want), (size + 4 * np.abs(want)) * U)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("V", [70, 5000, 70001])
+@pytest.mark.parametrize("scale", [3e38, 1e30, 1e6, 1e-6, 1e-30, 1e-38])
+def test_gradient_at_temperatures_of_any_size(V, scale, dtype):
+    """The difference of two logits, scale log2(e), their product and the difference with rlog are rounded: five halves of a step.
+    Probabilities below 2^-126 may be zero, times the scale, and times their logarithm below 128."""
+    x = draw((4, V), 1, dtype, 2.0)
+    x[1, V // 2] = x[1].max()
+    x[2] = x[2] * 1e30
+    x[3, 1:] = -INF
+    targets = torch.stack([x[0].argmax(), x[1].argmax(), x[2].argmin(), torch.zeros((), dtype=torch.int64, device=DEV)])
+    scale = float(np.float32(scale))
+    out = forward(x, targets, 0, scale)
+    dlogp, dH = draw((4,), 3, F32).clamp(-1, 1), draw((4,), 4, F32).clamp(-1, 1) / 300
+    dx = backward(x, targets, out["rmax"], out["rlog"], dlogp, scale, out["entropy"], dH)
+    check_backward(x, targets, out["rmax"], out["rlog"], dlogp, scale, out["entropy"], dH, dx, 5, 2 * TINY * max(1.0, scale))
 
 
 def test_gradient_against_differences():
