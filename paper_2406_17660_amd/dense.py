@@ -104,10 +104,13 @@ class TokenLoss:
 
     def backward(self, dlogp, dentropy=None, in_place=True):
         """The gradient of the logits from that of logp (and of the entropies, if forward() gave them): written over the
-        logits, or into a new tensor."""
+        logits, so that it is had once, or into a new tensor."""
+        assert self.given is not None, "no forward pass, or its logits are written over"
         logits, targets, entropy = self.given
         assert dentropy is None or entropy, "the forward pass left no entropies"
         T = logits.shape[0]
+        if in_place:
+            self.given = None
         return grass.logp_backward(logits, targets, self.rmax[:T], self.rlog[:T], dlogp, logits if in_place else torch.empty_like(logits),
                                    self.scale, entropy=self.entropy[:T] if dentropy is not None else None, dentropy=dentropy)
 

@@ -89,11 +89,14 @@ def test_embedding_and_loss_against_autograd(shared):
     embedding = Embedding(E, T + 9, scale, dE=dhead if shared else None)
     norm, loss = NormLayer(n, T + 9, torch.float32, "rms"), TokenLoss(T + 9, V, torch.float32, 0.8)
     y = norm.forward(embedding.forward(tokens))
-    logp, H = loss.forward(y @ head.t(), targets, entropy=True)
+    logits = y @ head.t()
+    logp, H = loss.forward(logits, targets, entropy=True)
     logp, H = logp.clone(), H.clone()
     kept = loss.backward(dlogp, dH, in_place=False)
     dlogits = loss.backward(dlogp, dH)
-    assert torch.equal(kept, dlogits) and dlogits.data_ptr() == loss.given[0].data_ptr()
+    assert torch.equal(kept, dlogits) and dlogits.data_ptr() == logits.data_ptr()
+    with pytest.raises(AssertionError):  # the logits are gone
+        loss.backward(dlogp, dH)
     torch.mm(dlogits.t(), y, out=dhead)
     embedding.backward(norm.backward(dlogits @ head), accumulate=shared)
 
