@@ -45,6 +45,8 @@
  *     by the kernels.)
  *   - No call records a memset or an event (the _timed call excepted) or allocates, so
  *     calls can be captured into a HIP graph.
+ *   - A workspace serves one call at a time: calls that may run together (on two streams, or in two
+ *     graphs whose replays overlap) need one each.
  */
 #ifndef GRASS_H
 #define GRASS_H

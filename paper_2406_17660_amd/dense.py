@@ -2,7 +2,7 @@
 probabilities at its two ends, and AdamW for the parameters that no projection covers (embeddings, output head, gains).
 
 Like `layer.py` this owns buffers and issues library calls in order; every step is a HIP kernel
-behind `grass.*`.
+behind `grass.*`.  An object's buffers serve one stream, and one graph's replay, at a time.
 """
 import torch
 
