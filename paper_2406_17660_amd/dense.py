@@ -95,11 +95,11 @@ class TokenLoss:
 
     def forward(self, logits, targets, entropy=False):
         """The targets' log probabilities (and the rows' entropies): views that the next forward pass writes over."""
-        T = logits.shape[0]
+        T, self.given = logits.shape[0], None  # (a refused call leaves no pass to go backward from)
         assert T <= self.T
-        self.given = logits, targets, entropy
         logp, H = self.logp[:T], self.entropy[:T] if entropy else None
         grass.logp_forward(logits, targets, logp, self.ws, self.scale, entropy=H, rmax=self.rmax[:T], rlog=self.rlog[:T])
+        self.given = logits, targets, entropy
         return (logp, H) if entropy else logp
 
     def backward(self, dlogp, dentropy=None, in_place=True):

@@ -1,0 +1,57 @@
+"""What the drivers of the embedding, the norms and the log probabilities keep between their calls, and what they refuse
+(CPU only: the library's calls are replaced by ones that accept, or refuse, whatever they are given)."""
+import pytest
+import torch
+
+from paper_2406_17660_amd import grass
+from paper_2406_17660_amd.dense import TokenLoss
+
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+class Refused(Exception):
+    pass
+
+
+@pytest.fixture
+def library(monkeypatch):
+    """The calls that were made, by name; those named in `refuse` raise."""
+    class Calls(list):
+        refuse = ()
+    calls = Calls()
+
+    def stand_in(name, result):
+        def f(*args, **kw):
+            if name in calls.refuse:
+                raise Refused(name)
+            calls.append(name)
+            return args[result]
+        monkeypatch.setattr(grass, name, f)
+    for name, result in (("embed_forward", 2), ("embed_backward", 2), ("logp_forward", 2), ("logp_backward", 5), ("norm_forward", 4),
+                         ("norm_backward", 5)):
+        stand_in(name, result)
+    return calls
+
+
+def loss_and_batch():
+    return TokenLoss(8, 12, F32, device="cpu"), torch.zeros(5, 12), torch.zeros(5, dtype=torch.int64), torch.zeros(5)
+
+
+@pytest.mark.parametrize("how", ["by the library", "for its length"])
+def test_no_gradient_after_a_refused_forward_pass_of_the_loss(library, how):
+    """rmax and rlog are still those of the batch before: with the new logits they would give a wrong gradient."""
+    loss, logits, targets, dlogp = loss_and_batch()
+    loss.forward(logits, targets)
+    if how == "by the library":
+        library.refuse = ("logp_forward",)
+        with pytest.raises(Refused):
+            loss.forward(torch.ones(5, 12), targets)
+    else:
+        with pytest.raises(AssertionError):
+            loss.forward(torch.ones(9, 12), torch.zeros(9, dtype=torch.int64))
+    with pytest.raises(AssertionError):
+        loss.backward(dlogp)
+    assert "logp_backward" not in library
+    library.refuse = ()
+    loss.forward(logits, targets)
+    assert loss.backward(dlogp) is logits
