@@ -109,10 +109,12 @@ class TokenLoss:
         logits, targets, entropy = self.given
         assert dentropy is None or entropy, "the forward pass left no entropies"
         T = logits.shape[0]
+        dlogits = grass.logp_backward(logits, targets, self.rmax[:T], self.rlog[:T], dlogp,
+                                      logits if in_place else torch.empty_like(logits), self.scale,
+                                      entropy=self.entropy[:T] if dentropy is not None else None, dentropy=dentropy)
         if in_place:
             self.given = None
-        return grass.logp_backward(logits, targets, self.rmax[:T], self.rlog[:T], dlogp, logits if in_place else torch.empty_like(logits),
-                                   self.scale, entropy=self.entropy[:T] if dentropy is not None else None, dentropy=dentropy)
+        return dlogits
 
 
 class AdamW:

@@ -55,3 +55,15 @@ def test_no_gradient_after_a_refused_forward_pass_of_the_loss(library, how):
     library.refuse = ()
     loss.forward(logits, targets)
     assert loss.backward(dlogp) is logits
+
+
+def test_a_refused_gradient_of_the_loss_leaves_the_logits_for_another(library):
+    loss, logits, targets, dlogp = loss_and_batch()
+    loss.forward(logits, targets)
+    library.refuse = ("logp_backward",)
+    with pytest.raises(Refused):
+        loss.backward(dlogp)
+    library.refuse = ()
+    assert loss.backward(dlogp) is logits
+    with pytest.raises(AssertionError):  # now they are written over
+        loss.backward(dlogp)
