@@ -67,13 +67,16 @@ class Embedding:
 
     def forward(self, ids, dtype=None):
         """The tokens' rows in a new tensor of E's type, or of `dtype`."""
-        assert ids.shape[0] <= self.T
+        T, self.ids = ids.shape[0], None  # (a refused call leaves no pass to go backward from)
+        assert T <= self.T
+        Y = torch.empty((T, self.E.shape[1]), dtype=dtype or self.E.dtype, device=self.E.device)
+        grass.embed_forward(self.E, ids, Y, self.scale)
         self.ids = ids
-        return grass.embed_forward(self.E, ids, torch.empty((ids.shape[0], self.E.shape[1]), dtype=dtype or self.E.dtype,
-                                                            device=self.E.device), self.scale)
+        return Y
 
     def backward(self, dY, accumulate=False):
         """self.dE from the gradient of what forward() gave; added to what it holds where accumulate is true."""
+        assert self.ids is not None, "no forward pass"
         return grass.embed_backward(dY, self.ids, self.dE, self.ws, self.scale, accumulate)
 
     def parameters(self):

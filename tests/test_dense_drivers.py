@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_2406_17660_amd import grass
-from paper_2406_17660_amd.dense import TokenLoss
+from paper_2406_17660_amd.dense import Embedding, TokenLoss
 
 F32, BF16 = torch.float32, torch.bfloat16
 
@@ -67,3 +67,19 @@ def test_a_refused_gradient_of_the_loss_leaves_the_logits_for_another(library):
     assert loss.backward(dlogp) is logits
     with pytest.raises(AssertionError):  # now they are written over
         loss.backward(dlogp)
+
+
+@pytest.mark.parametrize("how", ["no pass", "by the library", "for its length"])
+def test_no_gradient_of_the_embedding_without_a_forward_pass(library, how):
+    layer, dY = Embedding(torch.zeros(12, 6), 8), torch.zeros(5, 6)
+    if how != "no pass":
+        layer.forward(torch.zeros(5, dtype=torch.int64))
+        library.refuse = ("embed_forward",) if how == "by the library" else ()
+        with pytest.raises((Refused, AssertionError)):
+            layer.forward(torch.ones(9 if how == "for its length" else 5, dtype=torch.int64))
+    with pytest.raises(AssertionError, match="forward pass"):
+        layer.backward(dY)
+    assert "embed_backward" not in library
+    library.refuse = ()
+    layer.forward(torch.zeros(5, dtype=torch.int64))
+    assert layer.backward(dY) is layer.dE and layer.backward(dY, accumulate=True) is layer.dE
