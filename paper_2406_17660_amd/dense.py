@@ -63,6 +63,9 @@ class Embedding:
         V, n = E.shape
         self.E, self.T, self.scale, self.ids = E, T, scale, None
         self.dE = torch.zeros((V, n), dtype=torch.float32, device=E.device) if dE is None else dE
+        # (by the gradient's rows the kernels tell tokens from padding: with fewer of them than E has, tokens would be lost)
+        assert self.dE.shape == E.shape and self.dE.device == E.device, "the gradient has E's shape and device"
+        grass.dtype_code(self.dE.dtype)
         self.ws = grass.workspace(grass.embed_backward_workspace(T, V, n), E.device)
 
     def forward(self, ids, dtype=None):

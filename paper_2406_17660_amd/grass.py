@@ -210,11 +210,17 @@ def _stream():
 _DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
 
 
+def dtype_code(dtype) -> int:
+    """F32 or BF16 of a torch type; a TypeError for any other."""
+    code = _DTYPES.get(dtype)
+    if code is None:
+        raise TypeError(f"unsupported dtype {dtype}")
+    return code
+
+
 def _dtype(t: torch.Tensor) -> int:
     code = _DTYPES.get(t.dtype)
-    if code is None:
-        raise TypeError(f"unsupported dtype {t.dtype}")
-    return code
+    return dtype_code(t.dtype) if code is None else code
 
 
 def _mat(t: torch.Tensor):

@@ -83,3 +83,19 @@ def test_no_gradient_of_the_embedding_without_a_forward_pass(library, how):
     library.refuse = ()
     layer.forward(torch.zeros(5, dtype=torch.int64))
     assert layer.backward(dY) is layer.dE and layer.backward(dY, accumulate=True) is layer.dE
+
+
+@pytest.mark.parametrize("dE", [torch.zeros(11, 6), torch.zeros(13, 6), torch.zeros(12, 5), torch.zeros(72), torch.zeros(1, 12, 6),
+                                torch.zeros(12, 6, device="meta")])
+def test_a_given_gradient_has_the_embeddings_shape_and_device(dE):
+    """One of fewer rows would lose the tokens beyond them, which then count as padding."""
+    with pytest.raises(AssertionError, match="gradient"):
+        Embedding(torch.zeros(12, 6), 8, dE=dE)
+
+
+def test_a_given_gradient_of_the_embedding_of_either_type_is_kept():
+    for dtype in (F32, BF16):
+        dE = torch.zeros((12, 6), dtype=dtype)
+        assert Embedding(torch.zeros((12, 6), dtype=BF16), 8, dE=dE).parameters()[0][1] is dE
+    with pytest.raises(TypeError):
+        Embedding(torch.zeros(12, 6), 8, dE=torch.zeros(12, 6).half())
