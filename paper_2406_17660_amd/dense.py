@@ -20,7 +20,7 @@ class NormLayer:
 
     def __init__(self, n, T, dtype, kind="rms", bias=False, eps=1e-5, device="cuda"):
         self.n, self.T, self.kind, self.eps = n, T, NORMS[kind], eps
-        dt = grass.F32 if dtype == torch.float32 else grass.BF16
+        dt = grass.dtype_code(dtype)
         f32 = dict(dtype=torch.float32, device=device)
         self.gain, self.dgain = torch.ones(n, **f32), torch.zeros(n, **f32)
         self.bias = torch.zeros(n, **f32) if bias else None
@@ -96,7 +96,7 @@ class TokenLoss:
         self.T, self.scale = T, scale
         f32 = dict(dtype=torch.float32, device=device)
         self.logp, self.rmax, self.rlog, self.entropy = (torch.empty(T, **f32) for _ in range(4))
-        self.ws = grass.workspace(grass.logp_forward_workspace(T, V, 0, grass.F32 if dtype == torch.float32 else grass.BF16), device)
+        self.ws = grass.workspace(grass.logp_forward_workspace(T, V, 0, grass.dtype_code(dtype)), device)
         self.given = None
 
     def forward(self, logits, targets, entropy=False):

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_2406_17660_amd import grass
-from paper_2406_17660_amd.dense import Embedding, TokenLoss
+from paper_2406_17660_amd.dense import Embedding, NormLayer, TokenLoss
 
 F32, BF16 = torch.float32, torch.bfloat16
 
@@ -99,3 +99,14 @@ def test_a_given_gradient_of_the_embedding_of_either_type_is_kept():
         assert Embedding(torch.zeros((12, 6), dtype=BF16), 8, dE=dE).parameters()[0][1] is dE
     with pytest.raises(TypeError):
         Embedding(torch.zeros(12, 6), 8, dE=torch.zeros(12, 6).half())
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float64, torch.int32, torch.uint16])
+def test_types_that_no_kernel_takes_are_refused_at_construction(dtype):
+    """They would count as bf16, and fail, or find a workspace of another size, in the first call alone."""
+    with pytest.raises(TypeError):
+        TokenLoss(8, 12, dtype, device="cpu")
+    with pytest.raises(TypeError):
+        NormLayer(12, 8, dtype, device="cpu")
+    for dtype in (F32, BF16):
+        TokenLoss(8, 12, dtype, device="cpu"), NormLayer(12, 8, dtype, device="cpu")
