@@ -33,17 +33,18 @@ class NormLayer:
 
     def forward(self, X, R=None):
         """The norm of X (of X + R, the residual stream, which is kept as self.H) in a new tensor."""
-        T = X.shape[0]
+        T, self.H = X.shape[0], None  # (a refused call leaves no pass to go backward from)
         assert T <= self.T
-        Y = torch.empty_like(X)
-        self.H = X if R is None else torch.empty_like(X)
-        grass.norm_forward(X, self.gain, self.bias, self.eps, Y, self.kind, R=R, H=None if R is None else self.H,
+        Y, H = torch.empty_like(X), None if R is None else torch.empty_like(X)
+        grass.norm_forward(X, self.gain, self.bias, self.eps, Y, self.kind, R=R, H=H,
                            mean=None if self.mean is None else self.mean[:T], rstd=self.rstd[:T])
+        self.H = X if R is None else H
         return Y
 
     def backward(self, dY, dR=None):
         """The gradient of what forward() read, in a new tensor, plus dR, the residual stream's gradient from
         behind this layer; self.dgain and self.dbias receive the parameters' gradients."""
+        assert self.H is not None, "no forward pass"
         T = dY.shape[0]
         dX = torch.empty_like(dY)
         return grass.norm_backward(dY, self.H, self.gain, None if self.mean is None else self.mean[:T], self.rstd[:T], dX,

@@ -110,3 +110,23 @@ def test_types_that_no_kernel_takes_are_refused_at_construction(dtype):
         NormLayer(12, 8, dtype, device="cpu")
     for dtype in (F32, BF16):
         TokenLoss(8, 12, dtype, device="cpu"), NormLayer(12, 8, dtype, device="cpu")
+
+
+@pytest.mark.parametrize("how", ["no pass", "by the library", "for its length"])
+@pytest.mark.parametrize("residual", [False, True])
+def test_no_gradient_of_the_norm_without_a_forward_pass(library, residual, how):
+    """rstd (and mean) are still those of the batch before."""
+    layer, dY = NormLayer(6, 8, F32, device="cpu"), torch.zeros(5, 6)
+    if how != "no pass":
+        layer.forward(torch.zeros(5, 6))
+        library.refuse = ("norm_forward",) if how == "by the library" else ()
+        X = torch.ones(9 if how == "for its length" else 5, 6)
+        with pytest.raises((Refused, AssertionError)):
+            layer.forward(X, R=X if residual else None)
+    with pytest.raises(AssertionError, match="forward pass"):
+        layer.backward(dY)
+    assert "norm_backward" not in library
+    library.refuse = ()
+    X = torch.zeros(5, 6)
+    layer.forward(X)
+    assert layer.H is X and layer.backward(dY).shape == (5, 6)
