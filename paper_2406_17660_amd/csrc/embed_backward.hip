@@ -67,6 +67,22 @@ __device__ __forceinline__ Step step_of(Place p, bool there, int shift, int bits
     return s;
 }
 
+// Where the place of a step goes; the counter of its digit, which the wavefront's lanes share, moves on.  In the next step another
+// lane may lead the digit: the fences keep its access behind this one's (they cost no instruction; a wavefront's accesses to LDS are
+// served in order).
+__device__ __forceinline__ uint32_t take_place(uint32_t* next, const Step& s) {
+    const uint32_t at = next[s.digit];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (s.leads()) next[s.digit] = at + __popcll(s.same);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    return at + s.before();
+}
+// The same for a step that is only counted.
+__device__ __forceinline__ void count_place(uint32_t* next, const Step& s) {
+    if (s.leads()) next[s.digit] += __popcll(s.same);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+
 // f(step) over the wavefront's share of the workgroup's chunk, as often as asked.  kSteps: its steps where they stay in
 // registers; 0: any number of them, read again each time.
 template <int kSteps>
@@ -152,15 +168,6 @@ __device__ __forceinline__ void places_of_digits(uint32_t (&next)[kSortWaves][kM
     __syncthreads();
 }
 
-// Where the place of a step goes; the counter of its digit moves on.
-__device__ __forceinline__ uint32_t take_place(uint32_t* next, const Step& s) {
-    const uint32_t at = next[s.digit];
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    if (s.leads()) next[s.digit] = at + __popcll(s.same);
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    return at + s.before();
-}
-
 template <int kSteps>
 __global__ __launch_bounds__(kSortThreads) void scatter_kernel(SortArgs a) {
     __shared__ uint32_t next[kSortWaves][kMostBins], before[kSortThreads], all[kSortThreads], sums[kSortWaves];
@@ -180,9 +187,7 @@ __global__ __launch_bounds__(kSortThreads) void scatter_kernel(SortArgs a) {
     for (uint32_t k = group; k < kSortWaves; k += groups) next[k][digit] = 0;
     mine.arrive();
     __syncthreads();
-    mine.each([&](const Step& s) {
-        if (s.leads()) next[wave][s.digit] += __popcll(s.same);
-    });
+    mine.each([&](const Step& s) { count_place(next[wave], s); });
     if (threadIdx.x < bins)
         for (uint32_t g = 1; g < groups; ++g) {
             b += before[threadIdx.x + g * bins];
@@ -284,9 +289,7 @@ __global__ __launch_bounds__(kSortThreads) void order_kernel(SortArgs a) {
     };
     __syncthreads();
     if (lane == 0) atomicAdd(&lower, below);
-    each([&](const Step& s) {
-        if (s.leads()) next[wave][s.digit] += __popcll(s.same);
-    });
+    each([&](const Step& s) { count_place(next[wave], s); });
     __syncthreads();
     uint32_t count = 0;
     if (threadIdx.x < kRange) {
