@@ -670,6 +670,9 @@ grass_status grass_logp_backward(const void* logits, grass_dtype dt, int64_t T, 
  *   GRASS_TEST_UNALIGNED_X   1: an X in any position beside an aligned left operand (or the other way round)
  *                            takes the 256 tile's kernel for it from the first K tile and row tile on, and nothing
  *                            is copied into aligned rows
+ *   GRASS_TEST_MOST_BLOCKS   k > 0: the kernels of the embedding and of the log probabilities that walk over rows or
+ *                            pieces do so in at most k workgroups (which otherwise take some 2^20 before any of them
+ *                            takes a second turn)
  * Errors: DTYPE for an unknown option. */
 typedef enum {
     GRASS_TEST_GEMM_TILE = 0,
@@ -679,7 +682,8 @@ typedef enum {
     GRASS_TEST_MAX_K_SLICES = 4,
     GRASS_TEST_NO_NARROW_GATHER = 5,
     GRASS_TEST_RUN_TILE = 6,
-    GRASS_TEST_UNALIGNED_X = 7
+    GRASS_TEST_UNALIGNED_X = 7,
+    GRASS_TEST_MOST_BLOCKS = 8
 } grass_test_option;
 grass_status grass_set_test_option(grass_test_option option, int value);
 

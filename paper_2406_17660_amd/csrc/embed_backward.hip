@@ -676,8 +676,6 @@ Room room_of(int64_t T, int64_t V, int64_t n) {
     return r;
 }
 
-unsigned grid(int64_t blocks, int64_t most) { return static_cast<unsigned>(blocks < most ? blocks : most); }
-
 // Workgroups for so many pieces, and for rows of zeros.
 template <typename TY>
 void divide(SumArgs& a, int64_t pieces, bool accumulate) {
@@ -695,7 +693,7 @@ bool large(const SumArgs& a) { return static_cast<double>(a.V) * a.n * sizeof(TE
 template <typename TY, typename TE>
 void launch_few(SumArgs a, const Tokens& ids, bool accumulate, hipStream_t s) {
     divide<TY>(a, a.T, accumulate);
-    const unsigned blocks = grid(a.blocks, kMostBlocks);
+    const unsigned blocks = walking_grid(a.blocks);
     if (accumulate) few_kernel<TY, TE, true, false><<<blocks, kSumThreads, 0, s>>>(a, ids);
     else if (large<TE>(a)) few_kernel<TY, TE, false, true><<<blocks, kSumThreads, 0, s>>>(a, ids);
     else few_kernel<TY, TE, false, false><<<blocks, kSumThreads, 0, s>>>(a, ids);
@@ -710,11 +708,11 @@ void launch_sums(SumArgs a, hipStream_t s) {
     // into fp32 65536 x 512 68.5 / 57.0 / 68.3, 65536 x 1024 95.3 / 93.9 / 91.7, 65536 x 2048 150 / 148 / 146, 8192 x 1024 36.0 / 37.9 /
     // 43.3, 8192 x 2048 59.2 / 63.2 / 77.7.
     const bool out = large<TE>(a), in = static_cast<double>(a.T) * a.n * sizeof(TY) > kStreamed;
-    const unsigned blocks = grid(a.blocks, kMostBlocks);
+    const unsigned blocks = walking_grid(a.blocks);
     if (kPiece == 32 && in && out) sum_kernel<TY, TE, kPiece, kAccumulate, kPiece == 32, true><<<blocks, kSumThreads, 0, s>>>(a);
     else if (out) sum_kernel<TY, TE, kPiece, kAccumulate, false, true><<<blocks, kSumThreads, 0, s>>>(a);
     else sum_kernel<TY, TE, kPiece, kAccumulate, false, false><<<blocks, kSumThreads, 0, s>>>(a);
-    if (joins) join_kernel<TE, kPiece, kAccumulate><<<grid(joins, 8 * kUnits), kJoinThreads, 0, s>>>(a);
+    if (joins) join_kernel<TE, kPiece, kAccumulate><<<walking_grid(joins, 8 * kUnits), kJoinThreads, 0, s>>>(a);
 }
 
 }  // namespace

@@ -88,7 +88,7 @@ void launch(const void* E, int64_t n, int64_t lde, const Tokens& ids, int64_t T,
     constexpr int N = sizeof(TE) == 4 && sizeof(TY) == 4 ? 4 : 8;
     const LookupArgs a{E, Y, lde, ldy, T, static_cast<int>(n), ids, scale, Divisor(static_cast<uint32_t>((n + N - 1) / N))};
     const int64_t blocks = (T * a.vectors.d + kThreads * kEach - 1) / (kThreads * kEach);
-    const unsigned grid = static_cast<unsigned>(blocks < kMostBlocks ? blocks : kMostBlocks);
+    const unsigned grid = walking_grid(blocks);
     const double touched = static_cast<double>(T < ids.V ? T : ids.V) * n * sizeof(TE);
     const bool once = static_cast<double>(T) * n * sizeof(TY) + touched > kStreamed;
     const auto go = [&](auto copy) {

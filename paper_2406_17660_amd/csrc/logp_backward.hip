@@ -108,7 +108,7 @@ void launch(BackwardArgs a, hipStream_t s) {
         typedef decltype(shape) S;
         a.pieces = static_cast<int>((vectors + S::TPR * S::V - 1) / (S::TPR * S::V));
         const int64_t blocks = (a.T * a.pieces + S::kRows - 1) / S::kRows;
-        const unsigned grid = static_cast<unsigned>(blocks < kMostBlocks ? blocks : kMostBlocks);
+        const unsigned grid = walking_grid(blocks);
         if (a.dentropy) once ? backward_kernel<T, S, true, true><<<grid, 256, 0, s>>>(a) : backward_kernel<T, S, true, false><<<grid, 256, 0, s>>>(a);
         else once ? backward_kernel<T, S, false, true><<<grid, 256, 0, s>>>(a) : backward_kernel<T, S, false, false><<<grid, 256, 0, s>>>(a);
     };

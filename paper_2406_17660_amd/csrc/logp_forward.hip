@@ -554,7 +554,7 @@ void launch(const ForwardArgs& a, hipStream_t s) {
     by_width<T>(len, [&](auto shape) {
         typedef decltype(shape) S;
         const int64_t blocks = (a.T * a.parts + S::kRows - 1) / S::kRows;
-        const unsigned grid = static_cast<unsigned>(blocks < kMostBlocks ? blocks : kMostBlocks);
+        const unsigned grid = walking_grid(blocks);
         const bool once = static_cast<double>(a.T) * a.V * sizeof(T) > kStreamed;
         const auto go = [&](auto top, auto entropy, auto stream) {
             forward_kernel<T, S, decltype(top)::value, decltype(entropy)::value, decltype(stream)::value><<<grid, S::B, 0, s>>>(a);
@@ -563,7 +563,7 @@ void launch(const ForwardArgs& a, hipStream_t s) {
         const auto with_top = [&](auto top) { a.entropy ? with_entropy(top, std::true_type{}) : with_entropy(top, std::false_type{}); };
         a.top ? with_top(std::true_type{}) : with_top(std::false_type{});
     });
-    if (a.parts > 1) join_kernel<T><<<static_cast<unsigned>(a.T < kMostBlocks ? a.T : kMostBlocks), kJoin, 0, s>>>(a);
+    if (a.parts > 1) join_kernel<T><<<walking_grid(a.T), kJoin, 0, s>>>(a);
 }
 
 }  // namespace

@@ -1,6 +1,6 @@
-// Token numbers of 32 or 64 bits, and what the passes over logits share.
+// Token numbers of 32 or 64 bits, and what the kernels that walk over rows and the passes over logits share.
 #pragma once
-#include "common.hpp"
+#include "elem.hpp"
 
 namespace grass {
 namespace {
@@ -17,6 +17,13 @@ struct Tokens {
     }
 };
 inline Tokens tokens(const void* p, grass_index idt, int64_t V) { return {p, idt == GRASS_I64, static_cast<uint32_t>(V)}; }
+
+// The grid of a kernel that walks over the work of so many blocks: one workgroup for each, or `most` that take several turns.
+inline unsigned walking_grid(int64_t blocks, int64_t most = kMostBlocks) {
+    const int64_t forced = test_option(GRASS_TEST_MOST_BLOCKS);
+    if (forced > 0 && forced < most) most = forced;
+    return static_cast<unsigned>(blocks < most ? blocks : most);
+}
 
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945f;
 // scale log2(e), at most the largest number there is (0 times it is 0)

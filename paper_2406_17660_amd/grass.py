@@ -21,7 +21,7 @@ SEL_TOPR, SEL_UNIFORM, SEL_MULTI_NORM, SEL_MULTI_NORM2 = 0, 1, 2, 3
 SCALE_PAPER, SCALE_ONE, SCALE_INV_SQRT_RQ = 0, 1, 2
 DY_TxM, DY_MxT = 0, 1
 TEST_GEMM_TILE, TEST_FUSED_STATS, TEST_PACK_MXT, TEST_NO_PAIRS, TEST_MAX_K_SLICES = 0, 1, 2, 3, 4
-TEST_NO_NARROW_GATHER, TEST_RUN_TILE, TEST_UNALIGNED_X = 5, 6, 7
+TEST_NO_NARROW_GATHER, TEST_RUN_TILE, TEST_UNALIGNED_X, TEST_MOST_BLOCKS = 5, 6, 7, 8
 CALL_CGRAD, CALL_STEP, CALL_DENSE = range(3)
 NORM_LAYER, NORM_RMS = 0, 1
 I32, I64 = 0, 1
