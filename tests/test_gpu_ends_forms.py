@@ -106,3 +106,131 @@ def test_gradient_of_the_embedding_in_few_workgroups(few_blocks, T, V, n, dt, gd
     was = draw((V, n), 3, gdt) if accumulate else torch.full((V, n), float("nan"), dtype=gdt, device=DEV)
     want, got = (f(lambda: embed_backward(dY, ids, was.clone(), 0.5, accumulate)) for f in (lambda g: g(), few_blocks))
     assert bool(torch.isfinite(want.float()).all()) and same_bits(got, want)
+
+
+# ---------------------------------------------------------------- large calls: the streaming hint
+# Forward and backward passes carry it from 128 MiB on, the gradient of the embedding also where dE is above 32 MiB.  Such arrays are
+# compared on the card, in 64 bits, some rows at a time; the tolerances are those of the tests of each operator.
+STREAMED = 128 << 20
+
+
+def half_step(dtype):
+    return torch.finfo(dtype).eps / 2 if dtype == BF16 else 0.0
+
+
+def rows_at_a_time(T, n):
+    step = max(1, (1 << 25) // n)
+    return [slice(a, min(a + step, T)) for a in range(0, T, step)]
+
+
+def check_statistics(x, targets, scale, out):
+    """As derived for the forward pass: with E = entropy - rlog the sum of exponentials is off by SUM, log p by SUM + 4 U (|d| + rlog), the
+    entropy by SUM (1 + E) + 4 U (rlog + E)."""
+    V = x.shape[1]
+    for r in rows_at_a_time(*x.shape):
+        z = x[r].double()
+        m = z.amax(1, keepdim=True)
+        d = (z - m) * scale
+        rlog = d.exp().sum(1).log()
+        E = -((d - rlog.view(-1, 1)).exp() * d).sum(1)
+        SUM = (264 + 3 * E + rlog) * U
+        given = d.gather(1, targets[r].view(-1, 1))[:, 0]
+        assert torch.equal(out["rmax"][r].double(), m[:, 0])
+        assert bool(((out["rlog"][r].double() - rlog).abs() <= SUM).all())
+        assert bool(((out["logp"][r].double() - (given - rlog)).abs() <= SUM + 4 * U * (given.abs() + rlog)).all())
+        if out["entropy"] is not None:
+            assert bool(((out["entropy"][r].double() - (rlog + E)).abs() <= SUM * (1 + E) + 4 * U * (rlog + E)).all())
+        if out["top_idx"] is not None:
+            order = (x[r].float() + 0.0).view(torch.int32)
+            order = torch.where(order < 0, order ^ 0x7FFFFFFF, order).long() * (1 << 32) - torch.arange(V, device=DEV)
+            idx = torch.topk(order, out["top_idx"].shape[1], dim=1).indices
+            assert torch.equal(out["top_idx"][r].long(), idx)
+            best = d.gather(1, idx)
+            off = SUM.view(-1, 1) + 4 * U * (best.abs() + rlog.view(-1, 1))
+            assert bool(((out["top_logp"][r].double() - (best - rlog.view(-1, 1))).abs() <= off).all())
+
+
+def check_gradient_of_logits(x, targets, scale, out, dlogp, dentropy, dx):
+    """With rmax and rlog as they are given, p is off by (4 (|d| + rlog) + 8) U of itself."""
+    for r in rows_at_a_time(*x.shape):
+        col = lambda v: v[r].double().view(-1, 1)  # noqa: E731
+        rlog, H, g = col(out["rlog"]), col(out["entropy"]), col(dlogp)
+        h = torch.zeros_like(g) if dentropy is None else col(dentropy)
+        d = (x[r].double() - col(out["rmax"])) * scale
+        l = d - rlog
+        p = l.exp()
+        want = -p * (g + h * (l + H))
+        arg = d.abs() + rlog
+        rel = (4 * arg + 8) * U
+        size = p * (g.abs() * (rel + 2 * U) + h.abs() * ((l.abs() + H) * (rel + 4 * U) + 4 * U * (arg + l.abs() + H)))
+        j = targets[r].view(-1, 1)
+        want.scatter_add_(1, j, g)
+        size.scatter_add_(1, j, 4 * U * g.abs())
+        want, size = want * scale, size * scale
+        off = size + 2 * U * want.abs() + half_step(dx.dtype) * (want.abs() + size) + 2.0 ** -120 * (1 + g.abs() + h.abs())
+        assert bool(((dx[r].double() - want).abs() <= off).all())
+
+
+# one V in each shape, as above, and enough rows
+@pytest.mark.parametrize("dtype,V", [(BF16, v) for v in (100, 300, 1000, 2048, 4001, 8192, 16000, 20480, 32000, 50001, 140003)] +
+                         [(F32, v) for v in (50, 256, 500, 1024, 2001, 4096, 8000, 10240, 16384, 50001, 70001)])
+def test_log_probabilities_of_large_calls(dtype, V):
+    T = STREAMED // (V * dtype.itemsize) + 17
+    x, targets = draw((T, V), 1, dtype, 2.0), whole((T,), 2, V)
+    dlogp, dH = draw((T,), 3, F32), draw((T,), 4, F32)
+    for top, entropy in ((9, True), (9, False), (0, False), (0, True)):
+        out = forward(x, targets, top, 0.5, entropy=entropy)
+        check_statistics(x, targets, 0.5, out)
+    for d in (None, dH):
+        dx = backward(x, targets, out["rmax"], out["rlog"], dlogp, 0.5, None if d is None else out["entropy"], d)
+        check_gradient_of_logits(x, targets, 0.5, out, dlogp, d, dx)
+    dlogp[::3], dH[::3], targets[1::3] = 0.0, 0.0, -1  # rows that are not read
+    x[::3] = float("nan")
+    again = backward(x, targets, out["rmax"], out["rlog"], dlogp, 0.5, out["entropy"], dH)
+    assert not again[::3].any() and torch.equal(again[2::3], dx[2::3])
+
+
+@pytest.mark.parametrize("edt,ydt", [(F32, F32), (F32, BF16), (BF16, F32), (BF16, BF16)])
+@pytest.mark.parametrize("T,n", [(1100000, 70), (40000, 4096), (20001, 5461)])
+@pytest.mark.parametrize("scale", [1.0, 0.37])
+def test_lookup_of_large_calls(T, n, edt, ydt, scale):
+    """One fp32 product, rounded once to its type; with a scale of one and one type the bits as they are."""
+    V = 20000
+    E, ids = draw((V, n), 1, edt), whole((T,), 2, V + 2) - 1
+    Y = torch.full((T, n), float("nan"), dtype=ydt, device=DEV)
+    assert Y.nbytes > STREAMED
+    grass.embed_forward(E, ids, Y, scale)
+    there = ((ids >= 0) & (ids < V)).view(-1, 1)
+    exact = torch.tensor(scale, dtype=F32).double().item()
+    for r in rows_at_a_time(T, n):
+        want = E[ids[r].clamp(0, V - 1)].double() * exact * there[r]
+        if scale == 1.0 and edt == ydt:
+            assert torch.equal(Y[r].double(), want)
+        else:
+            assert bool(((Y[r].double() - want).abs() <= (U + half_step(ydt) * (1 + U)) * want.abs()).all())
+
+
+# dY and dE streamed, in pieces of 32; dE alone, in pieces of 32 and of 8; dE of a few places
+@pytest.mark.parametrize("T,V,n", [(40000, 20000, 2048), (40000, 32000, 640), (5000, 9000, 2048), (100, 9000, 2048), (40011, 19001, 2051),
+                                   (5003, 9001, 2051), (101, 9001, 2051)])
+@pytest.mark.parametrize("dt,gdt", [(F32, F32), (F32, BF16), (BF16, F32), (BF16, BF16)])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_gradient_of_the_embedding_of_large_calls(T, V, n, dt, gdt, accumulate):
+    """Sums of c rows: (c + 2) half steps of fp32 of the magnitudes, and one rounding to the type."""
+    dY, ids = draw((T, n), 1, dt), (torch.rand(T, device=DEV, generator=torch.Generator(DEV).manual_seed(2)) ** 3 * (V + 1)).long() - 1
+    ids[T // 4:T // 3] = V // 2
+    was = draw((V, n), 3, gdt) if accumulate else torch.full((V, n), float("nan"), dtype=gdt, device=DEV)
+    dE = embed_backward(dY, ids, was.clone(), 0.5, accumulate)
+    assert dE.nbytes > 1 << 25
+    row = torch.where((ids >= 0) & (ids < V), ids, V)
+    count = row.bincount(minlength=V + 1)[:V].view(-1, 1)
+    want, size = (torch.zeros((V + 1, n), dtype=torch.float64, device=DEV) for _ in range(2))
+    for r in rows_at_a_time(T, n):
+        want.index_add_(0, row[r], dY[r].double() * 0.5)
+        size.index_add_(0, row[r], dY[r].double().abs() * 0.5)
+    want, size = want[:V], size[:V]
+    if accumulate:
+        want, size = want + was.double(), size + was.double().abs()
+        assert torch.equal(dE[count[:, 0] == 0], was[count[:, 0] == 0])
+    off = (count + 2) * U * size
+    assert bool(((dE.double() - want).abs() <= off + half_step(gdt) * (want.abs() + off)).all())
