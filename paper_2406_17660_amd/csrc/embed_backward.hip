@@ -733,7 +733,8 @@ grass_status launch_embed_backward(const void* dY, grass_dtype dt, int64_t lddy,
     const int64_t ranges = (V + kRange - 1) / kRange;
     // One kernel does as much as there are ranges times places.  us of whole calls with it / with the radix sort, 64 bf16 features:
     // 32000 tokens 16384 places 24.4 / 45.6, 32768 39.5 / 45.7, 65536 51.9 / 52.8; 128000 tokens 16384 places 29.4 / 36.4, 65536 66.8 / 61.2.
-    if (T > kFew && T <= 32768 && ranges * T <= (1 << 23) && ranges <= 65536) {  // (a grid has fewer than 2^32 threads)
+    if (T > kFew && T <= 32768 && ranges * T <= (1 << 23)) {
+        static_assert((1 << 23) / kFew < (int64_t{1} << 32) / kSortThreads, "a grid has fewer than 2^32 threads");
         order_kernel<<<static_cast<unsigned>(ranges), kSortThreads, 0, s>>>(sort);
     } else if (T > kFew) {
         const unsigned grid = static_cast<unsigned>(r.blocks);

@@ -234,3 +234,17 @@ def test_gradient_of_the_embedding_of_large_calls(T, V, n, dt, gdt, accumulate):
         assert torch.equal(dE[count[:, 0] == 0], was[count[:, 0] == 0])
     off = (count + 2) * U * size
     assert bool(((dE.double() - want).abs() <= off + half_step(gdt) * (want.abs() + off)).all())
+
+
+# the radix sort: chunks in registers, several passes, chunks read again; and the one-kernel ordering
+@pytest.mark.parametrize("T,V", [(65536, 32000), (20000, 262145), (33000, 1), (600000, 700), (1000, 300), (30000, 9)])
+def test_token_numbers_of_32_bits(T, V):
+    """Rows of small whole numbers, whose sums are exact in any order; padding of either sign, the largest numbers among it."""
+    ids = whole((T,), 1, V).int()
+    ids[::13] = torch.tensor([-1, V, -100, (1 << 31) - 1, -(1 << 31)], dtype=torch.int32, device=DEV).repeat(T)[:len(ids[::13])]
+    dY = whole((T, 5), 2, 9).to(BF16) - 4
+    there = (ids >= 0) & (ids < V)
+    want = torch.zeros((V, 5), dtype=torch.float64, device=DEV).index_add_(0, ids[there].long(), dY[there].double())
+    dE = embed_backward(dY, ids, torch.full((V, 5), float("nan"), device=DEV))
+    assert torch.equal(dE.double(), want)
+    assert torch.equal(embed_backward(dY, ids.long(), torch.full((V, 5), float("nan"), device=DEV)), dE)
