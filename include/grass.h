@@ -593,7 +593,9 @@ grass_status grass_embed_forward(const void* E, grass_dtype edt, int64_t V, int6
  * occur are zeros, or with accumulate neither read nor written; rows of dY whose ids[t] names no token are
  * not read.  The sums are fp32, in an order that depends on the token numbers and sizes alone, so
  * that equal calls give equal bits.  `ws` must hold grass_embed_backward_workspace(T, V, n) bytes (which
- * grow with T, so that one workspace serves shorter batches, too), 16-byte aligned.  T = 0 writes zeros,
+ * grow with T, so that one workspace serves shorter batches, too; most of them are two fp32 rows for every 8 tokens
+ * of a short batch or 32 of a long one, 134 MB at T = 131072 and n = 4096; calls of up to 256 tokens ask for them as
+ * well, and use none), 16-byte aligned.  T = 0 writes zeros,
  * or with accumulate nothing; V, n >= 1; scale is finite.
  * Errors: NULL, SHAPE (also an address that is not a multiple of its type's size), DTYPE, WORKSPACE. */
 size_t grass_embed_backward_workspace(int64_t T, int64_t V, int64_t n);

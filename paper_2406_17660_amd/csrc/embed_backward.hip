@@ -7,7 +7,7 @@
 // their order depends on the tokens alone.
 //
 // Bound by memory: dY is read once, dE written once.  Measured, whole calls: 131072 x 4096 bf16 into 32000 bf16 rows 313 us (1.34 GB,
-// 4.3 TB/s; the sums 265, ordering 28, frequent tokens 22); 65536 x 512 bf16 into fp32 rows 55 us (the sums 25, ordering 25,
+// 4.3 TB/s; the sums 265, ordering 28, frequent tokens 19); 65536 x 512 bf16 into fp32 rows 55 us (the sums 25, ordering 25,
 // frequent tokens 5.5); 2047 x 5461 bf16 added to fp32 rows 28.
 #include "elem.hpp"
 #include "tokens.hpp"
@@ -444,7 +444,9 @@ __device__ __forceinline__ void sum_piece(const SumArgs& a, int64_t item) {
             for (int g = 0; g < kGroups; ++g)
                 if (some(g)) at[g].template load<kIn>(row, x[k][g]);
         }
-        if constexpr (kAccumulate)  // (the rows that are added to are on their way at the same time)
+        // (The rows that are added to are on their way at the same time.  Their registers, bf16 added to fp32, leave room for three
+        // wavefronts a SIMD, where six fit without.)
+        if constexpr (kAccumulate)
 #pragma unroll
             for (int k = 0; k < kAhead; ++k) {
                 const int j = i + k;
@@ -496,7 +498,8 @@ __global__ __launch_bounds__(kSumThreads) void sum_kernel(SumArgs a) {
 
 // Up to kFew places: a wavefront to each (and tile) looks at all of them, and the one at a token's first place adds up its rows.  One
 // launch, without an order: 64 or 256 places and 64 features, added, 13.1 and 14.9 -> 6.9 us, what the call takes the host; 256 places and
-// 4096 features 15.9 -> 6.9; 64 places into 32000 x 2048 fp32 56.7 -> 51.9, rows of zeros (5.0 TB/s).
+// 4096 features 15.9 -> 6.9; 64 places into 32000 x 2048 fp32 56.7 -> 51.9, rows of zeros (5.0 TB/s).  A frequent token is one
+// wavefront's work: 256 places, a third of them one token's, 12 us (512 features) and 14 (4096), all of them 38.
 constexpr int kFew = 256;
 
 template <typename TY, typename TE, bool kAccumulate, bool kOut>
@@ -572,7 +575,8 @@ __global__ __launch_bounds__(kSumThreads) void few_kernel(SumArgs a, Tokens ids)
 }
 
 // The partial sums of a long token, 256 columns a workgroup at a time: each wavefront adds up a share of the pieces in order, and the
-// shares are added in order.
+// shares are added in order.  A very frequent token leaves narrow rows' sums to few workgroups: whole calls with Zipf's law alone / one
+// token in 30 % of the places besides / in all of them, 65536 x 512 bf16 into fp32 55 / 69 / 99 us, 131072 x 4096 into bf16 315 / 325 / 375.
 constexpr int kJoinThreads = 256, kJoinWaves = kJoinThreads / kWave;
 
 template <typename TE, int kPiece, bool kAccumulate>

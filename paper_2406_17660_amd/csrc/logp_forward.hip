@@ -49,7 +49,9 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return r;
 }
 
-// Threads that share a row, V vectors of 16 bytes each, in blocks of B; alternatives are chosen among up to kCap logits.
+// Threads that share a row, V vectors of 16 bytes each, in blocks of B; alternatives are chosen among up to kCap logits.  Eight wavefronts
+// a SIMD fit in all shapes without alternatives, and in those of 256 and 512 threads with them, where the bf16 ones of eight vectors keep
+// two registers in memory; of 64 threads with alternatives six fit (LDS), with eight vectors five (registers).
 template <int TPR_, int V_>
 struct Shape {
     static constexpr int TPR = TPR_, V = V_, B = TPR_ < 256 ? 256 : TPR_, kRows = B / TPR_, kCap = TPR_ < 256 ? 512 : 1024;
@@ -534,6 +536,10 @@ int parts_of(int64_t V, grass_dtype dt) { return dt == GRASS_F32 ? parts_of<floa
 
 // us with the largest parts at 512 threads / 1024 / 256: 1025 x 50001 bf16 with 5 alternatives 51 / 69 / 55, 256 x 128000 fp32 with 20
 // 55 / 63 / 98, 32768 x 32000 bf16 304 / - / 367 (all before later steps).  One row of 32000 bf16 by 1024 threads 11.0 us, by 512 9.6.
+// Otherwise the fewest threads and vectors that hold a row.  us of 32768 bf16 rows without / with entropies and 20 alternatives by the
+// shape taken, and by a larger one: 2048 logits 31 / 63, by 256 threads 50 / 136; 4096 46 / 95, by 256 threads 60 / 154; 8192 97 / 187, by
+// 512 threads 128 / 296; 16384 162 / 261, by 512 threads 179 / 352; 18000 with five vectors 201 / 365, with eight 203 / 385; 20480 212 / 380
+// and 217 / 400.
 template <typename T, typename F>
 void by_width(int64_t len, F&& f) {
     const int64_t vectors = (len * static_cast<int64_t>(sizeof(T)) + 15) / 16;
